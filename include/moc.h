@@ -230,6 +230,100 @@ int moc_outer_reduced_layout(const moc_plan *plan, const int32_t *sel_shot, int3
  * stream keeps (tok_map: DEVICE int32; out: DEVICE [H][n_out][d] bf16). */
 int moc_gather_tokens(const moc_plan *plan, const void *X, const int32_t *tok_map, int32_t n_out, void *out, void *stream);
 
+/* ---- Beside the stream's sparse attention: what a layer does to its queries and keys before it, and the cross attention behind
+ * it (the DiT block of the paper's experiments: Wan-2.1 style per-head norm, 3-D rotary positions, cross attention to the prompt).
+ *
+ * Rows of d consecutive values, one per (head, token): row (h, t) begins at data + h * head_stride + t * token_stride elements.
+ * data is a DEVICE pointer, 16-byte aligned; both strides are multiples of 16 bytes, below 2^39 elements, and keep the rows apart:
+ * either a token's heads lie within token_stride (a projection's output, [token][head][d], or a part of a fused one) or a head's
+ * tokens lie within head_stride ([head][token][d]).  The stride of a dimension of extent 1 is not looked at.  MOC_ERR_ALIGN /
+ * MOC_ERR_SHAPE otherwise: broadcast tensors (a stride of 0) are refused, shared heads are stated by their count. */
+typedef struct moc_rows {
+    void *data;
+    int64_t head_stride, token_stride;
+} moc_rows;
+
+#define MOC_BF16 0
+#define MOC_FP32 1
+
+#define MOC_ROPE_HALVES 0x1u  /* channel j is turned with channel j + n_pairs; otherwise 2 j with 2 j + 1 */
+
+/* A position rotation with up to four axes (time, height, width), as a list of pairs of channels: pair j is turned by
+ * pos[token][pair_axis[j]] * pair_freq[j] radians.  Channels from 2 n_pairs on are not turned; n_pairs = 0: no rotation.  The arrays
+ * are HOST memory, read during moc_rope_create only.  The object holds no device memory and serves every device. */
+typedef struct moc_rope_problem {
+    int32_t head_dim;            /* d: 64 or 128                                                              */
+    int32_t n_pairs;             /* 0 <= n_pairs <= d / 2; with MOC_ROPE_HALVES a multiple of 8               */
+    int32_t n_axes;              /* positions per token, 1..4 (not looked at without pairs)                   */
+    uint32_t flags;              /* MOC_ROPE_*                                                                */
+    float eps;                   /* of the norm, >= 0                                                         */
+    const int32_t *pair_axis;    /* [n_pairs], 0 <= axis < n_axes                                             */
+    const double *pair_freq;     /* [n_pairs], radians per step, |freq| <= 1e6                                */
+} moc_rope_problem;
+
+typedef struct moc_rope moc_rope;
+
+int moc_rope_create(const moc_rope_problem *problem, moc_rope **out);
+int moc_rope_destroy(moc_rope *rope);
+int moc_rope_workspace_bytes(const moc_rope *rope, size_t *bytes);     /* for moc_norm_rope_bwd */
+
+/* Norm of every head's row of the queries and of the keys, then the rotation, in one pass:
+ *     u = x / sqrt(mean(x^2) + eps) * w  (w NULL: u = x),  out = the rotation of u by the token's angles, rounded once to bf16.
+ * x_type (MOC_BF16, MOC_FP32) is the type of q and k; q_out, k_out are bf16, in the layout that moc_chunk_pool / moc_route /
+ * moc_attend take when they are contiguous [H][L][d].  w_q, w_k: DEVICE fp32 [d], shared by all heads.  pos: DEVICE int32
+ * [n_tokens][n_axes] (any value; angles are formed in 64 bits).  n_k_heads may be 0: k, w_k, k_out are not looked at then.  n_tokens may be 0.
+ * An output may be its own input where type and strides are the same; no other overlap. */
+int moc_norm_rope(const moc_rope *rope, int x_type, int32_t n_tokens, int32_t n_q_heads, int32_t n_k_heads, const int32_t *pos,
+                  const moc_rows *q, const float *w_q, const moc_rows *q_out, const moc_rows *k, const float *w_k,
+                  const moc_rows *k_out, void *stream);
+
+/* Its backward pass: from dq_out, dk_out (bf16, the gradients of the outputs) to dq, dk (x_type) and, where there is a norm, dw_q, dw_k
+ * (fp32 [d], overwritten: the sum over heads and tokens, in an order that depends on the sizes alone).  q, k: the forward's
+ * inputs (not looked at without a norm; dw must be NULL then).  ws: moc_rope_workspace_bytes, 256-byte aligned, used
+ * during the call only.  dq may be dq_out or q where type and strides are the same; no other overlap. */
+int moc_norm_rope_bwd(const moc_rope *rope, int x_type, int32_t n_tokens, int32_t n_q_heads, int32_t n_k_heads, const int32_t *pos,
+                      const moc_rows *q, const float *w_q, const moc_rows *dq_out, const moc_rows *dq, float *dw_q, const moc_rows *k,
+                      const float *w_k, const moc_rows *dk_out, const moc_rows *dk, float *dw_k, void *ws, void *stream);
+
+/* Cross attention: the stream's queries to encoder states of another length (the prompt's), segment by segment - a segment is a shot
+ * with its own prompt, or a sequence of a batch.  Segment s: the queries [q_off[s], q_off[s+1]) attend to the states
+ * [k_off[s], k_off[s] + k_len[s]), k_len[s] <= k_off[s+1] - k_off[s] (k_len NULL: all of them); what is left of a segment's states is padding.
+ * Either part may be empty.  q_off, k_off, k_len are HOST pointers, read during moc_cross_create only. */
+typedef struct moc_cross_problem {
+    int32_t n_heads, n_kv_heads;          /* query head h reads key head h / (n_heads / n_kv_heads); n_heads <= 65535 */
+    int32_t head_dim, n_segments;         /* d in {64, 128}; n_segments >= 0                                        */
+    float softmax_scale;                  /* 0 => 1/sqrt(d)                                                         */
+    const int32_t *q_off, *k_off;         /* [n_segments + 1], from 0 on, non-decreasing                            */
+    const int32_t *k_len;                 /* [n_segments] or NULL                                                   */
+} moc_cross_problem;
+
+typedef struct moc_cross moc_cross;
+
+/* As moc_plan_create: validates the tables, derives the work of every launch and uploads it to the current device. */
+int moc_cross_create(const moc_cross_problem *problem, moc_cross **out);
+int moc_cross_destroy(moc_cross *cross);
+
+/* Bytes of caller-owned scratch (256-byte aligned) for moc_cross_attend (with_bwd = 0) or both calls (with_bwd = 1).  It carries
+ * nothing from one call to the next but the status; calls that may overlap on the GPU need one each. */
+int moc_cross_workspace_bytes(const moc_cross *cross, int with_bwd, size_t *bytes);
+
+/* O = softmax(scale Q K^T) V over the segment's states, lse (fp32, [n_heads][q_off[n_segments]] contiguous) = ln of the sum of
+ * exp(scale q.k).  Q, O: bf16 rows of n_heads heads and q_off[n_segments] tokens (at least: rows behind them are neither read nor written);
+ * K, V: of n_kv_heads heads and k_off[n_segments] tokens.  A query without states gets O = 0 and lse = -inf.  Padding is
+ * not looked at: it may hold anything.  Products in bf16, fp32 accumulation and softmax. */
+int moc_cross_attend(const moc_cross *cross, const moc_rows *Q, const moc_rows *K, const moc_rows *V, const moc_rows *O, float *lse,
+                     void *ws, void *stream);
+
+/* Its backward pass: dQ, dK, dV (bf16) from dO; the gradients of shared key heads are summed over their query heads, in an order that
+ * depends on the problem alone.  Padding, and states whose segment has no queries, get zeros.  P and dS are rounded to bf16 before
+ * their contractions, as in moc_attend_bwd. */
+int moc_cross_attend_bwd(const moc_cross *cross, const moc_rows *Q, const moc_rows *K, const moc_rows *V, const moc_rows *O,
+                         const float *lse, const moc_rows *dO, const moc_rows *dQ, const moc_rows *dK, const moc_rows *dV, void *ws,
+                         void *stream);
+
+/* As moc_get_status, of the last moc_cross_attend or moc_cross_attend_bwd on ws. */
+int moc_cross_get_status(const moc_cross *cross, const void *ws, void *stream, int *device_status, int *detail);
+
 /* How many kernel launches the library's calls have enqueued since it was loaded (plan creation, which fills a
  * table with one, not counted). */
 int64_t moc_launch_count(void);

@@ -19,6 +19,20 @@ class MocError(RuntimeError):
         self.code = code
 
 
+class _Rows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("head_stride", C.c_int64), ("token_stride", C.c_int64)]
+
+
+class _RopeProblem(C.Structure):
+    _fields_ = [("head_dim", C.c_int32), ("n_pairs", C.c_int32), ("n_axes", C.c_int32), ("flags", C.c_uint32), ("eps", C.c_float),
+                ("pair_axis", C.c_void_p), ("pair_freq", C.c_void_p)]
+
+
+class _CrossProblem(C.Structure):
+    _fields_ = [("n_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("n_segments", C.c_int32),
+                ("softmax_scale", C.c_float), ("q_off", C.c_void_p), ("k_off", C.c_void_p), ("k_len", C.c_void_p)]
+
+
 class _Problem(C.Structure):
     _fields_ = [("n_heads", C.c_int32), ("n_tokens", C.c_int32), ("head_dim", C.c_int32),
                 ("n_chunks", C.c_int32), ("top_k", C.c_int32), ("win_back", C.c_int32), ("win_fwd", C.c_int32),
@@ -68,6 +82,18 @@ def load_library():
     lib.moc_debug_shared_key_tiles.argtypes = [C.POINTER(_Problem), i32, i32, C.POINTER(i32), vp, vp, C.POINTER(sz)]
     lib.moc_attend.argtypes = [vp] * 9
     lib.moc_attend_bwd.argtypes = [vp] * 13
+    rows = C.POINTER(_Rows)
+    lib.moc_rope_create.argtypes = [C.POINTER(_RopeProblem), C.POINTER(vp)]
+    lib.moc_rope_destroy.argtypes = [vp]
+    lib.moc_rope_workspace_bytes.argtypes = [vp, C.POINTER(sz)]
+    lib.moc_norm_rope.argtypes = [vp, i32, C.c_int32, C.c_int32, C.c_int32, vp] + [rows, vp, rows] * 2 + [vp]
+    lib.moc_norm_rope_bwd.argtypes = [vp, i32, C.c_int32, C.c_int32, C.c_int32, vp] + [rows, vp, rows, rows, vp] * 2 + [vp, vp]
+    lib.moc_cross_create.argtypes = [C.POINTER(_CrossProblem), C.POINTER(vp)]
+    lib.moc_cross_destroy.argtypes = [vp]
+    lib.moc_cross_workspace_bytes.argtypes = [vp, i32, C.POINTER(sz)]
+    lib.moc_cross_attend.argtypes = [vp] + [rows] * 4 + [vp] * 3
+    lib.moc_cross_attend_bwd.argtypes = [vp] + [rows] * 4 + [vp] + [rows] * 4 + [vp] * 2
+    lib.moc_cross_get_status.argtypes = [vp, vp, vp, C.POINTER(i32), C.POINTER(i32)]
     lib.moc_selected_pairs.argtypes = [vp, vp, vp, C.POINTER(C.c_int64)]
     lib.moc_get_status.argtypes = [vp, vp, vp, C.POINTER(i32), C.POINTER(i32)]
     lib.moc_launch_count.restype = C.c_int64
@@ -246,3 +272,180 @@ class MocPlan:
         self.moc_route(Q, desc, sel, ws)
         self.moc_attend(Q, K, V, sel, O, lse, ws)
         return desc, sel, O, lse, ws
+
+
+def _rows(t, heads, tokens, d, dtype, name):
+    """A [heads][tokens][d] tensor of any strides as the library takes it."""
+    if t.dtype != dtype or t.dim() != 3 or t.shape[0] != heads or t.shape[1] != tokens or t.shape[2] != d:
+        raise MocError(-2, f"moc error -2: {name} is {t.dtype} {tuple(t.shape)}, not {dtype} {(heads, tokens, d)}")
+    if t.stride(2) != 1:
+        raise MocError(-2, f"moc error -2: the channels of {name} are not consecutive")
+    _on_current(t, name)
+    return _Rows(t.data_ptr(), t.stride(0), t.stride(1))
+
+
+def _on_current(t, name):
+    if not t.is_cuda or t.device.index != torch._C._cuda_getDevice():
+        raise MocError(-6, f"moc error -6: {name} is on {t.device}, which is not the current device")
+
+
+def _table(t, shape, dtype, name):
+    """The address of a contiguous tensor, or NULL."""
+    if t is None:
+        return None
+    if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous():
+        raise MocError(-2, f"moc error -2: {name} is {t.dtype} {tuple(t.shape)}, not contiguous {dtype} {shape}")
+    _on_current(t, name)
+    return t.data_ptr()
+
+
+def _scratch(ws, n_bytes):
+    if ws is None or ws.numel() * ws.element_size() < n_bytes or not ws.is_contiguous():
+        raise MocError(-5, f"moc error -5: a contiguous workspace of {n_bytes} bytes is needed")
+    _on_current(ws, "the workspace")
+    return ws.data_ptr()
+
+
+class MocRope:
+    """Owns a ``moc_rope``: the norm of every query and key head with the position rotation in one pass.  Queries, keys and their
+    outputs are [head][token][d] tensors of any strides (the channels consecutive), for instance parts of a fused projection
+    [token][head][d], transposed.
+
+    pair_axis, pair_freq: of every turned pair of channels the axis of its position, and radians per step."""
+
+    def __init__(self, head_dim, pair_axis=(), pair_freq=(), n_axes=None, eps=1e-6, halves=False):
+        self._lib = load_library()
+        self._h = C.c_void_p(0)
+        axis = np.ascontiguousarray(pair_axis, np.int32)
+        freq = np.ascontiguousarray(pair_freq, np.float64)
+        if axis.shape != freq.shape or axis.ndim != 1:
+            raise MocError(-2, "moc error -2: pair_axis and pair_freq are lists of the same length")
+        if n_axes is None:
+            n_axes = int(axis.max()) + 1 if len(axis) else 0
+        pr = _RopeProblem(int(head_dim), len(axis), int(n_axes), 0x1 if halves else 0, float(eps), axis.ctypes.data, freq.ctypes.data)
+        _check(self._lib.moc_rope_create(C.byref(pr), C.byref(self._h)))
+        self.d, self.n_axes = int(head_dim), int(n_axes) if len(axis) else 0
+        n = C.c_size_t(0)
+        _check(self._lib.moc_rope_workspace_bytes(self._h, C.byref(n)))
+        self._ws_bytes = int(n.value)
+
+    @classmethod
+    def from_axes(cls, head_dim, axis_dims, theta=10000.0, **kw):
+        """Axis a turns axis_dims[a] channels (an even number), its pair m by theta ** (-2 m / axis_dims[a]) a step; the axes' pairs
+        follow one another, and the channels behind them are not turned."""
+        if any(int(n) < 0 or int(n) % 2 for n in axis_dims):
+            raise MocError(-2, "moc error -2: an axis turns an even number of channels")
+        axis = [a for a, n in enumerate(axis_dims) for _ in range(int(n) // 2)]
+        freq = [float(theta) ** (-2.0 * m / int(n)) for n in axis_dims for m in range(int(n) // 2)]
+        return cls(head_dim, axis, freq, n_axes=len(axis_dims), **kw)
+
+    def close(self):
+        if self._h:
+            self._lib.moc_rope_destroy(self._h)
+            self._h = C.c_void_p(0)
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def workspace_bytes(self) -> int:
+        return self._ws_bytes
+
+    def new_workspace(self, device="cuda") -> torch.Tensor:
+        return torch.empty(self._ws_bytes, dtype=torch.uint8, device=device)
+
+    def _common(self, pos, q, k):
+        L = q.shape[1]
+        if q.dtype not in (torch.bfloat16, torch.float32):
+            raise MocError(-2, f"moc error -2: queries are bf16 or fp32, not {q.dtype}")
+        return (1 if q.dtype == torch.float32 else 0, L, q.shape[0], 0 if k is None else k.shape[0],
+                _table(pos, (L, self.n_axes), torch.int32, "pos") if self.n_axes else None)
+
+    def moc_norm_rope(self, pos, q, w_q, q_out, k=None, w_k=None, k_out=None):
+        """q_out (and k_out) <- norm and rotation of q (and k); pos: int32 [token][axis]; w_q, w_k: fp32 [d], or None for no norm."""
+        x_type, L, hq, hk, at = self._common(pos, q, k)
+        b16, d = torch.bfloat16, self.d
+        rk = (_rows(k, hk, L, d, q.dtype, "k"), _table(w_k, (d,), torch.float32, "w_k"), _rows(k_out, hk, L, d, b16, "k_out")) if hk else (None,) * 3
+        _check(self._lib.moc_norm_rope(self._h, x_type, L, hq, hk, at, _rows(q, hq, L, d, q.dtype, "q"), _table(w_q, (d,), torch.float32, "w_q"),
+                                       _rows(q_out, hq, L, d, b16, "q_out"), *rk, _stream()))
+
+    def moc_norm_rope_bwd(self, pos, q, w_q, dq_out, dq, dw_q, ws, k=None, w_k=None, dk_out=None, dk=None, dw_k=None):
+        """dq, dw_q (and dk, dw_k) <- from dq_out (and dk_out), the gradients of moc_norm_rope's outputs."""
+        x_type, L, hq, hk, at = self._common(pos, q, k)
+        b16, d, f32 = torch.bfloat16, self.d, torch.float32
+        rk = (None,) * 5
+        if hk:
+            rk = (_rows(k, hk, L, d, q.dtype, "k"), _table(w_k, (d,), f32, "w_k"), _rows(dk_out, hk, L, d, b16, "dk_out"),
+                  _rows(dk, hk, L, d, q.dtype, "dk"), _table(dw_k, (d,), f32, "dw_k"))
+        _check(self._lib.moc_norm_rope_bwd(self._h, x_type, L, hq, hk, at, _rows(q, hq, L, d, q.dtype, "q"), _table(w_q, (d,), f32, "w_q"),
+                                           _rows(dq_out, hq, L, d, b16, "dq_out"), _rows(dq, hq, L, d, q.dtype, "dq"), _table(dw_q, (d,), f32, "dw_q"),
+                                           *rk, _scratch(ws, self._ws_bytes), _stream()))
+
+
+class MocCross:
+    """Owns a ``moc_cross``: attention of a stream's segments (shots, or sequences of a batch) to encoder states of another
+    length.  q_off, k_off: [segments + 1] where each segment's queries and states begin; k_len: how many of them it has
+    (default: up to the next one's).  Tensors are [head][token][d], bf16, of any strides (the channels consecutive)."""
+
+    def __init__(self, n_heads, n_kv_heads, head_dim, q_off, k_off, k_len=None, softmax_scale=0.0):
+        self._lib = load_library()
+        self._h = C.c_void_p(0)
+        qo, ko = np.ascontiguousarray(q_off, np.int32), np.ascontiguousarray(k_off, np.int32)
+        kl = None if k_len is None else np.ascontiguousarray(k_len, np.int32)
+        if qo.ndim != 1 or len(qo) < 1 or ko.shape != qo.shape or (kl is not None and kl.shape != (len(qo) - 1,)):
+            raise MocError(-3, "moc error -3: segment tables have inconsistent lengths")
+        pr = _CrossProblem(int(n_heads), int(n_kv_heads), int(head_dim), len(qo) - 1, float(softmax_scale), qo.ctypes.data, ko.ctypes.data,
+                           None if kl is None else kl.ctypes.data)
+        _check(self._lib.moc_cross_create(C.byref(pr), C.byref(self._h)))
+        self.H, self.Hkv, self.d = int(n_heads), int(n_kv_heads), int(head_dim)
+        self.n_queries, self.n_states = int(qo[-1]), int(ko[-1])
+        self._ws_bytes = []
+        for with_bwd in (0, 1):
+            n = C.c_size_t(0)
+            _check(self._lib.moc_cross_workspace_bytes(self._h, with_bwd, C.byref(n)))
+            self._ws_bytes.append(int(n.value))
+
+    def close(self):
+        if self._h:
+            self._lib.moc_cross_destroy(self._h)
+            self._h = C.c_void_p(0)
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def workspace_bytes(self, with_bwd=False) -> int:
+        return self._ws_bytes[1 if with_bwd else 0]
+
+    def new_workspace(self, with_bwd=False, device="cuda") -> torch.Tensor:
+        return torch.empty(self.workspace_bytes(with_bwd), dtype=torch.uint8, device=device)
+
+    def _q(self, t, name):       # (a tensor may have more rows than the segments: those behind the last one's are left alone)
+        if t.dim() == 3 and t.shape[1] < self.n_queries:
+            raise MocError(-2, f"moc error -2: {name} has {t.shape[1]} rows, the segments {self.n_queries}")
+        return _rows(t, self.H, t.shape[1] if t.dim() == 3 else self.n_queries, self.d, torch.bfloat16, name)
+
+    def _k(self, t, name):
+        if t.dim() == 3 and t.shape[1] < self.n_states:
+            raise MocError(-2, f"moc error -2: {name} has {t.shape[1]} rows, the segments {self.n_states}")
+        return _rows(t, self.Hkv, t.shape[1] if t.dim() == 3 else self.n_states, self.d, torch.bfloat16, name)
+
+    def moc_cross_attend(self, Q, K, V, O, lse, ws):
+        """O, lse (fp32 [head][query]) <- attention of every segment's queries to its states."""
+        _check(self._lib.moc_cross_attend(self._h, self._q(Q, "Q"), self._k(K, "K"), self._k(V, "V"), self._q(O, "O"),
+                                          _table(lse, (self.H, self.n_queries), torch.float32, "lse"), _scratch(ws, self._ws_bytes[0]), _stream()))
+
+    def moc_cross_attend_bwd(self, Q, K, V, O, lse, dO, dQ, dK, dV, ws):
+        """dQ, dK, dV <- from dO, the gradient of O; O, lse: the forward's."""
+        _check(self._lib.moc_cross_attend_bwd(self._h, self._q(Q, "Q"), self._k(K, "K"), self._k(V, "V"), self._q(O, "O"),
+                                              _table(lse, (self.H, self.n_queries), torch.float32, "lse"), self._q(dO, "dO"), self._q(dQ, "dQ"),
+                                              self._k(dK, "dK"), self._k(dV, "dV"), _scratch(ws, self._ws_bytes[1]), _stream()))
+
+    def moc_cross_get_status(self, ws):
+        st, det = C.c_int(0), C.c_int(0)
+        _check(self._lib.moc_cross_get_status(self._h, _ptr(ws), _stream(), C.byref(st), C.byref(det)))
+        return int(st.value), int(det.value)

@@ -1143,7 +1143,7 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t
                                   const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
                                   CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
-int make_tmap_2d_bf16(CUtensorMap *map, const void *base, uint64_t rows, uint64_t cols, uint32_t box_rows) {
+static int encode_tmap(CUtensorMap *map, const void *base, int n_dims, const cuuint64_t *dims, const cuuint64_t *strides, const cuuint32_t *box) {
     static EncodeTiledFn fn = nullptr;
     if (!fn) {
         void *sym = nullptr;
@@ -1152,15 +1152,26 @@ int make_tmap_2d_bf16(CUtensorMap *map, const void *base, uint64_t rows, uint64_
         if (!sym || q != cudaDriverEntryPointSuccess) { set_cuda_error(cudaErrorUnknown, "cuTensorMapEncodeTiled not found"); return MOC_ERR_CUDA; }
         fn = (EncodeTiledFn)sym;
     }
-    cuuint64_t dims[2] = {cols, rows};
-    cuuint64_t strides[1] = {cols * 2};
-    cuuint32_t box[2] = {64, box_rows};
-    cuuint32_t estr[2] = {1, 1};
-    CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(base), dims, strides, box, estr,
+    const cuuint32_t estr[3] = {1, 1, 1};
+    CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, n_dims, const_cast<void *>(base), dims, strides, box, estr,
                     CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) { set_cuda_error(cudaErrorInvalidValue, "cuTensorMapEncodeTiled"); return MOC_ERR_CUDA; }
     return MOC_OK;
+}
+
+int make_tmap_2d_bf16(CUtensorMap *map, const void *base, uint64_t rows, uint64_t cols, uint32_t box_rows) {
+    const cuuint64_t dims[2] = {cols, rows}, strides[1] = {cols * 2};
+    const cuuint32_t box[2] = {64, box_rows};
+    return encode_tmap(map, base, 2, dims, strides, box);
+}
+
+int make_tmap_rows_bf16(CUtensorMap *map, const moc_rows *r, uint64_t heads, uint64_t rows, uint64_t cols, uint32_t box_rows) {
+    // (a dimension of extent 1 may have any stride: one that the encoding takes)
+    const cuuint64_t dims[3] = {cols, rows, heads};
+    const cuuint64_t strides[2] = {rows > 1 ? (uint64_t)r->token_stride * 2 : cols * 2, heads > 1 ? (uint64_t)r->head_stride * 2 : cols * 2};
+    const cuuint32_t box[3] = {64, box_rows, 1};
+    return encode_tmap(map, r->data, 3, dims, strides, box);
 }
 
 template <int D, bool LOADERS>

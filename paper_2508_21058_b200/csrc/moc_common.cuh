@@ -243,6 +243,20 @@ void layout_workspace(moc_plan *p);
 
 static inline bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 
+// Rows of a caller's tensor (moc_rows), `elem` bytes a value: what the header asks of their address and strides.
+static inline int check_rows(const moc_rows *r, int64_t heads, int64_t tokens, int d, int elem) {
+    if (!r) return MOC_ERR_NULL;
+    if (heads == 0 || tokens == 0) return MOC_OK;
+    if (!r->data) return MOC_ERR_NULL;
+    if (!aligned(r->data, 16)) return MOC_ERR_ALIGN;
+    const int64_t hs = heads > 1 ? r->head_stride : d, ts = tokens > 1 ? r->token_stride : d;
+    if (hs < d || ts < d || hs >= (1ll << 39) || ts >= (1ll << 39)) return MOC_ERR_SHAPE;
+    if (hs * elem % 16 != 0 || ts * elem % 16 != 0) return MOC_ERR_ALIGN;
+    const bool tokens_outside = tokens == 1 || (heads - 1) * hs + d <= ts;
+    const bool heads_outside = heads == 1 || (__int128)(tokens - 1) * ts + d <= hs;
+    return tokens_outside || heads_outside ? MOC_OK : MOC_ERR_SHAPE;
+}
+
 // kernels' host launchers (each returns a moc_status)
 int launch_chunk_pool(const moc_plan *p, const __nv_bfloat16 *K, float *desc, void *ws, cudaStream_t s);
 int launch_route(const moc_plan *p, const __nv_bfloat16 *Q, const float *desc, int32_t *sel, void *ws, cudaStream_t s);

@@ -1,0 +1,405 @@
+// Cross attention to encoder states of another length (moc_cross_attend, moc_cross_attend_bwd): the plan, the entry points and the small
+// kernels that put shares together.  The attention itself: moc_cross_fwd_tc.cu, moc_cross_dq_tc.cu, moc_cross_dkv_tc.cu.
+#include <string.h>
+
+#include <algorithm>
+#include <cmath>
+#include <new>
+
+#include "moc_cross.cuh"
+#include "moc_tc.cuh"
+
+namespace moc {
+
+static size_t up256(size_t x) { return (x + 255) / 256 * 256; }
+
+static int check_cross(const moc_cross_problem *pr) {
+    if (pr->n_heads < 1 || pr->n_heads > 65535 || pr->n_kv_heads < 1 || pr->n_heads % pr->n_kv_heads != 0) return MOC_ERR_SHAPE;
+    if (pr->head_dim != 64 && pr->head_dim != 128) return MOC_ERR_SHAPE;
+    if (pr->n_segments < 0 || !std::isfinite(pr->softmax_scale) || pr->softmax_scale < 0.f) return MOC_ERR_SHAPE;
+    if (!pr->q_off || !pr->k_off) return MOC_ERR_NULL;
+    if (pr->q_off[0] != 0 || pr->k_off[0] != 0) return MOC_ERR_CHUNK_TABLE;
+    for (int s = 0; s < pr->n_segments; ++s) {
+        if (pr->q_off[s + 1] < pr->q_off[s] || pr->k_off[s + 1] < pr->k_off[s]) return MOC_ERR_CHUNK_TABLE;
+        if (pr->k_len && (pr->k_len[s] < 0 || pr->k_len[s] > pr->k_off[s + 1] - pr->k_off[s])) return MOC_ERR_CHUNK_TABLE;
+    }
+    const int64_t Lq = pr->q_off[pr->n_segments], Lk = pr->k_off[pr->n_segments];
+    // (some to spare: a tile's last row, and a round of items, are worked out in 32 bits)
+    if (Lq * pr->n_heads >= (1ll << 31) - 1024 || Lk * pr->n_kv_heads >= (1ll << 31) - 1024) return MOC_ERR_SHAPE;
+    return MOC_OK;
+}
+
+// Shares of the keys.  With many items the longest-first walk balances the CTAs by itself; with few, and long key lists, an item is cut into
+// shares of `c` key tiles, whose results another launch puts together.  c is the one with the least estimated time, in key tiles of a
+// full item: the slowest CTA's walk, where an item costs 1.5 beside its tiles (its first loads and its results) and a tile 0.6 with a
+// single row tile, plus 3 for the second launch.
+static int share_tiles(const std::vector<CrossItem> &items, int H, int n_sm, int two_rows) {
+    int longest = 0;
+    for (const CrossItem &i : items) longest = std::max(longest, (i.n_keys + 127) / 128);
+    if (longest < 2 || items.size() * (size_t)H >= 4 * (size_t)n_sm) return std::max(longest, 1);
+    int best_c = longest;
+    double best = 1e300;
+    std::vector<double> cost;
+    for (int p = 1; p <= std::min(longest, 128); ++p) {
+        const int c = (longest + p - 1) / p;
+        cost.clear();
+        for (const CrossItem &i : items) {
+            const int nt = (i.n_keys + 127) / 128, n = std::max(1, (nt + c - 1) / c);
+            for (int x = 0; x < n; ++x) cost.push_back(1.5 + (i.rows > two_rows ? 1.0 : 0.6) * (nt * (x + 1) / n - nt * x / n));
+        }
+        std::sort(cost.begin(), cost.end(), [](double a, double b) { return a > b; });
+        double t = c < longest ? 3.0 : 0.0;
+        for (size_t at = 0; at < cost.size() * (size_t)H; at += n_sm) t += cost[at / H];
+        if (t < best) { best = t; best_c = c; }
+    }
+    return best_c;
+}
+
+// cuts the items into shares of at most c key tiles; the longest items first
+static void cut_items(std::vector<CrossItem> &items, std::vector<CrossMerge> &merges, int &slots, int c) {
+    std::vector<CrossItem> out;
+    for (const CrossItem &i : items) {
+        const int nt = (i.n_keys + 127) / 128, n = std::max(1, (nt + c - 1) / c);
+        if (n == 1) { out.push_back(i); continue; }
+        merges.push_back(CrossMerge{i.q0, i.rows, slots, n});
+        for (int x = 0; x < n; ++x) {
+            const int t0 = (int)((int64_t)nt * x / n), t1 = (int)((int64_t)nt * (x + 1) / n);
+            CrossItem p = i;
+            p.k0 = i.k0 + t0 * 128;
+            p.n_keys = std::min(i.n_keys, t1 * 128) - t0 * 128;
+            p.slot = slots++;
+            out.push_back(p);
+        }
+    }
+    std::stable_sort(out.begin(), out.end(), [](const CrossItem &a, const CrossItem &b) { return (a.n_keys + 127) / 128 > (b.n_keys + 127) / 128; });
+    items.swap(out);
+}
+
+static void derive_cross(moc_cross *c, const moc_cross_problem *pr) {
+    const int S = pr->n_segments;
+    c->H = pr->n_heads; c->Hkv = pr->n_kv_heads; c->g = pr->n_heads / pr->n_kv_heads; c->d = pr->head_dim;
+    c->Lq = pr->q_off[S]; c->Lk = pr->k_off[S];
+    c->scale = pr->softmax_scale != 0.f ? pr->softmax_scale : 1.f / std::sqrt((float)c->d);
+    auto keys = [&](int s) { return pr->k_len ? pr->k_len[s] : pr->k_off[s + 1] - pr->k_off[s]; };
+    for (int s = 0; s < S; ++s) {
+        for (int q = pr->q_off[s]; q < pr->q_off[s + 1]; q += kCrossRows)
+            c->items.push_back(CrossItem{q, std::min(kCrossRows, pr->q_off[s + 1] - q), pr->k_off[s], keys(s), -1, {}});
+        for (int q = pr->q_off[s]; q < pr->q_off[s + 1]; q += 128)
+            c->dq_items.push_back(CrossItem{q, std::min(128, pr->q_off[s + 1] - q), pr->k_off[s], keys(s), -1, {}});
+    }
+    cut_items(c->items, c->merges, c->slots, share_tiles(c->items, c->H, c->n_sm, 128));
+    cut_items(c->dq_items, c->dq_merges, c->dq_slots, share_tiles(c->dq_items, c->H, c->n_sm, 0));
+
+    // Key-stationary pass: all (key tile, query tile) pairs in a row, cut into equal stretches, one for every CTA (of two pairs at
+    // least); a key tile that lies in several stretches is a sum of slots.
+    struct Tile { int h, k0, keys, q0, q1; int64_t units; };
+    std::vector<Tile> tiles;
+    int64_t total = 0;
+    for (int h = 0; h < c->Hkv; ++h)
+        for (int s = 0; s < S; ++s) {
+            const int64_t units = (int64_t)c->g * ((pr->q_off[s + 1] - pr->q_off[s] + 127) / 128);
+            const int end = pr->k_off[s] + keys(s);
+            for (int k = pr->k_off[s]; k < pr->k_off[s + 1];) {
+                const int n = std::min(128, (k < end ? end : pr->k_off[s + 1]) - k);
+                if (k >= end || units == 0) c->sums.push_back(CrossSum{h, k, n, 0, 0, {}});
+                else { tiles.push_back(Tile{h, k, n, pr->q_off[s], pr->q_off[s + 1], units}); total += units; }
+                k += n;
+            }
+        }
+    const int64_t n_cta = std::min<int64_t>(c->n_sm, (total + 1) / 2);
+    size_t ti = 0;
+    int64_t base = 0;                                    // units before tile ti
+    c->piece_off.push_back(0);
+    for (int64_t b = 0; b < n_cta; ++b) {
+        int64_t at = total * b / n_cta;
+        const int64_t end = total * (b + 1) / n_cta;
+        while (at < end) {
+            const Tile &t = tiles[ti];
+            const int64_t upto = std::min(end, base + t.units);
+            c->pieces.push_back(CrossPiece{t.h, t.k0, t.keys, t.q0, t.q1, (int)(at - base), (int)(upto - base), -1});
+            at = upto;
+            if (at == base + t.units) { base += t.units; ++ti; }
+        }
+        c->piece_off.push_back((int)c->pieces.size());
+    }
+    for (size_t a = 0; a < c->pieces.size();) {
+        size_t e = a + 1;
+        while (e < c->pieces.size() && c->pieces[e].u0 != 0) ++e;
+        if (e - a > 1) {
+            c->sums.push_back(CrossSum{c->pieces[a].h, c->pieces[a].k0, c->pieces[a].keys, c->kv_slots, (int)(e - a), {}});
+            for (size_t x = a; x < e; ++x) c->pieces[x].slot = c->kv_slots++;
+        }
+        a = e;
+    }
+    CrossLayout &w = c->ws;
+    const size_t H = c->H, d = c->d;
+    w.status = 0;
+    w.part_o = 256;
+    w.part_lse = up256(w.part_o + 4 * H * c->slots * kCrossRows * d);
+    w.fwd_end = up256(w.part_lse + 4 * H * c->slots * kCrossRows);
+    w.delta = w.fwd_end;
+    w.part_dq = up256(w.delta + 4 * H * c->Lq);
+    w.part_kv = up256(w.part_dq + 4 * H * c->dq_slots * 128 * d);
+    w.bwd_end = up256(w.part_kv + 4 * 2 * (size_t)c->kv_slots * 128 * d);
+}
+
+// ---- delta_i = sum_x dO_ix O_ix, a warp a row pair: 16 lanes a row at d = 128, 8 at d = 64, 16 bytes a lane
+template <int D>
+__global__ void __launch_bounds__(256) cross_delta_kernel(CrossRows O, CrossRows dO, float *delta, int *status, int H, int Lq) {
+    constexpr int LPR = D / 8, RPW = 32 / LPR, U = 2;
+    if (blockIdx.x == 0 && threadIdx.x == 0) status[ST_STATUS] = status[ST_DETAIL] = 0;
+    const int lane = threadIdx.x & 31, chunk = lane % LPR;
+    const int64_t n = (int64_t)H * Lq;
+    for (int64_t r0 = ((int64_t)blockIdx.x * 8 + (threadIdx.x >> 5)) * (U * RPW); r0 < n; r0 += (int64_t)gridDim.x * 8 * (U * RPW)) {
+        uint4 a[U], b[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t r = r0 + u * RPW + lane / LPR;
+            a[u] = b[u] = make_uint4(0, 0, 0, 0);
+            if (r < n) {
+                const int h = (int)(r / Lq), t = (int)(r - (int64_t)h * Lq);
+                a[u] = *reinterpret_cast<const uint4 *>(O.row(h, t) + chunk * 8);
+                b[u] = *reinterpret_cast<const uint4 *>(dO.row(h, t) + chunk * 8);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t r = r0 + u * RPW + lane / LPR;
+            const uint32_t x[4] = {a[u].x, a[u].y, a[u].z, a[u].w}, y[4] = {b[u].x, b[u].y, b[u].z, b[u].w};
+            float v = 0.f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                v = fmaf(__uint_as_float(x[i] << 16), __uint_as_float(y[i] << 16), v);
+                v = fmaf(__uint_as_float(x[i] & 0xffff0000u), __uint_as_float(y[i] & 0xffff0000u), v);
+            }
+#pragma unroll
+            for (int o = LPR / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+            if (r < n && chunk == 0) delta[r] = v;
+        }
+    }
+}
+
+// ---- shares of the forward: O = sum_i w_i O_i / sum_i w_i, w_i = exp(lse_i - max lse); a warp a row
+template <int D>
+__global__ void __launch_bounds__(256) cross_merge_kernel(const CrossMerge *merges, const float *part_o, const float *part_lse, int slots,
+                                                          CrossRows O, float *lse, int Lq) {
+    const CrossMerge m = merges[blockIdx.x];
+    const int h = blockIdx.y, row = blockIdx.z * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    if (row >= m.rows) return;
+    const size_t at = ((size_t)h * slots + m.slot) * kCrossRows + row;
+    float big = -INFINITY;
+    for (int i = lane; i < m.n; i += 32) big = fmaxf(big, part_lse[at + (size_t)i * kCrossRows]);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, o));
+    constexpr int V = D / 32;
+    float acc[V] = {}, sum = 0.f;
+    for (int i = 0; i < m.n; ++i) {
+        const float w = __expf(part_lse[at + (size_t)i * kCrossRows] - big);
+        sum += w;
+        const float *src = part_o + (at + (size_t)i * kCrossRows) * D + lane * V;
+#pragma unroll
+        for (int x = 0; x < V; x += 2) {
+            const float2 v = *reinterpret_cast<const float2 *>(src + x);
+            acc[x] = fmaf(w, v.x, acc[x]);
+            acc[x + 1] = fmaf(w, v.y, acc[x + 1]);
+        }
+    }
+    const float inv = 1.f / sum;
+    uint32_t *dst = reinterpret_cast<uint32_t *>(O.row(h, m.q0 + row) + lane * V);
+#pragma unroll
+    for (int x = 0; x < V; x += 2) dst[x / 2] = tc::bf16x2(acc[x] * inv, acc[x + 1] * inv);
+    if (lane == 0) lse[(size_t)h * Lq + m.q0 + row] = big + __logf(sum);
+}
+
+// ---- shares of a gradient: out = sum of the slots, in their order; a warp a row
+template <int D>
+__device__ __forceinline__ void sum_row(const float *src, size_t stride, int n, __nv_bfloat16 *dst) {
+    constexpr int V = D / 32;
+    float acc[V] = {};
+    for (int i = 0; i < n; ++i)
+#pragma unroll
+        for (int x = 0; x < V; x += 2) {
+            const float2 v = *reinterpret_cast<const float2 *>(src + i * stride + x);
+            acc[x] += v.x;
+            acc[x + 1] += v.y;
+        }
+#pragma unroll
+    for (int x = 0; x < V; x += 2) reinterpret_cast<uint32_t *>(dst)[x / 2] = tc::bf16x2(acc[x], acc[x + 1]);
+}
+template <int D>
+__global__ void __launch_bounds__(256) cross_sum_dq_kernel(const CrossMerge *merges, const float *part, int slots, CrossRows dQ) {
+    const CrossMerge m = merges[blockIdx.x];
+    const int h = blockIdx.y, row = blockIdx.z * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    if (row < m.rows)
+        sum_row<D>(part + (((size_t)h * slots + m.slot) * 128 + row) * D + lane * (D / 32), (size_t)128 * D, m.n, dQ.row(h, m.q0 + row) + lane * (D / 32));
+}
+template <int D>
+__global__ void __launch_bounds__(256) cross_sum_kv_kernel(const CrossSum *sums, const float *part, CrossRows dK, CrossRows dV) {
+    const CrossSum m = sums[blockIdx.x];
+    const int side = blockIdx.y, row = blockIdx.z * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    if (row < m.rows)
+        sum_row<D>(part + (((size_t)m.slot * 2 + side) * 128 + row) * D + lane * (D / 32), (size_t)2 * 128 * D, m.n,
+                   (side ? dV : dK).row(m.h, m.k0 + row) + lane * (D / 32));
+}
+
+static int enter_cross(const moc_cross *c) {
+    if (!c) return MOC_ERR_NULL;
+    int dev = -1;
+    MOC_CUDA_TRY(cudaGetDevice(&dev));
+    return dev == c->device ? MOC_OK : MOC_ERR_ARCH;
+}
+static int check_ws(const void *ws) { return !ws ? MOC_ERR_WORKSPACE : aligned(ws, 256) ? MOC_OK : MOC_ERR_ALIGN; }
+
+}  // namespace moc
+
+using namespace moc;
+
+extern "C" int moc_cross_create(const moc_cross_problem *pr, moc_cross **out) {
+    if (!pr || !out) return MOC_ERR_NULL;
+    if (int r = check_cross(pr)) return r;
+    int dev = -1, cc = 0, n_sm = 0;
+    MOC_CUDA_TRY(cudaGetDevice(&dev));
+    MOC_CUDA_TRY(cudaDeviceGetAttribute(&cc, cudaDevAttrComputeCapabilityMajor, dev));
+    MOC_CUDA_TRY(cudaDeviceGetAttribute(&n_sm, cudaDevAttrMultiProcessorCount, dev));
+    if (cc != 10) return MOC_ERR_ARCH;
+    moc_cross *c = new (std::nothrow) moc_cross();
+    if (!c) return MOC_ERR_CUDA;
+    c->device = dev;
+    c->n_sm = n_sm;
+    try {                                                       // (the tables' memory)
+        derive_cross(c, pr);
+        size_t o = 0;
+        auto take = [&](size_t bytes) { const size_t at = o; o = up256(o + bytes); return at; };
+        const size_t a = take(sizeof(CrossItem) * c->items.size()), b = take(sizeof(CrossItem) * c->dq_items.size()),
+                     m = take(sizeof(CrossMerge) * c->merges.size()), dm = take(sizeof(CrossMerge) * c->dq_merges.size()),
+                     p = take(sizeof(CrossPiece) * c->pieces.size()), po = take(4 * c->piece_off.size()), su = take(sizeof(CrossSum) * c->sums.size());
+        std::vector<char> host(o);
+        auto up = [&](size_t at, const void *src, size_t bytes) { if (bytes) memcpy(host.data() + at, src, bytes); };
+        up(a, c->items.data(), sizeof(CrossItem) * c->items.size());
+        up(b, c->dq_items.data(), sizeof(CrossItem) * c->dq_items.size());
+        up(m, c->merges.data(), sizeof(CrossMerge) * c->merges.size());
+        up(dm, c->dq_merges.data(), sizeof(CrossMerge) * c->dq_merges.size());
+        up(p, c->pieces.data(), sizeof(CrossPiece) * c->pieces.size());
+        up(po, c->piece_off.data(), 4 * c->piece_off.size());
+        up(su, c->sums.data(), sizeof(CrossSum) * c->sums.size());
+        cudaError_t e = cudaMalloc(&c->d_blob, o);
+        if (e == cudaSuccess) {
+            // on a stream of its own: on the legacy stream the copy would wait for what the caller has under way there
+            cudaStream_t st = nullptr;
+            e = cudaStreamCreateWithFlags(&st, cudaStreamNonBlocking);
+            if (e == cudaSuccess) {
+                e = cudaMemcpyAsync(c->d_blob, host.data(), o, cudaMemcpyHostToDevice, st);
+                const cudaError_t e2 = cudaStreamSynchronize(st);
+                cudaStreamDestroy(st);
+                if (e == cudaSuccess) e = e2;
+            }
+        }
+        if (e != cudaSuccess) {
+            set_cuda_error(e, "cross attention tables");
+            if (c->d_blob) cudaFree(c->d_blob);
+            delete c;
+            return MOC_ERR_CUDA;
+        }
+        char *d = static_cast<char *>(c->d_blob);
+        c->d_items = (CrossItem *)(d + a); c->d_dq_items = (CrossItem *)(d + b);
+        c->d_merges = (CrossMerge *)(d + m); c->d_dq_merges = (CrossMerge *)(d + dm);
+        c->d_pieces = (CrossPiece *)(d + p); c->d_piece_off = (int32_t *)(d + po); c->d_sums = (CrossSum *)(d + su);
+    } catch (...) {
+        delete c;
+        return MOC_ERR_CUDA;
+    }
+    *out = c;
+    return MOC_OK;
+}
+
+extern "C" int moc_cross_destroy(moc_cross *c) {
+    if (!c) return MOC_ERR_NULL;
+    if (c->d_blob) cudaFree(c->d_blob);
+    delete c;
+    return MOC_OK;
+}
+
+extern "C" int moc_cross_workspace_bytes(const moc_cross *c, int with_bwd, size_t *bytes) {
+    if (!c || !bytes) return MOC_ERR_NULL;
+    *bytes = with_bwd ? c->ws.bwd_end : c->ws.fwd_end;
+    return MOC_OK;
+}
+
+extern "C" int moc_cross_attend(const moc_cross *c, const moc_rows *Q, const moc_rows *K, const moc_rows *V, const moc_rows *O, float *lse,
+                                void *ws, void *stream) {
+    moc::NvtxRange nvtx_range("moc_cross_attend");
+    if (int r = enter_cross(c)) return r;
+    for (const moc_rows *t : {Q, O}) if (int r = check_rows(t, c->H, c->Lq, c->d, 2)) return r;
+    for (const moc_rows *t : {K, V}) if (int r = check_rows(t, c->Hkv, c->Lk, c->d, 2)) return r;
+    if (c->Lq > 0 && !lse) return MOC_ERR_NULL;
+    if (!aligned(lse, 4)) return MOC_ERR_ALIGN;
+    if (int r = check_ws(ws)) return r;
+    cudaStream_t s = (cudaStream_t)stream;
+    if (c->Lq == 0) {
+        MOC_CUDA_TRY(cudaMemsetAsync(ws_ptr<int>(ws, c->ws.status), 0, 8, s));
+        return MOC_OK;
+    }
+    if (int r = launch_cross_fwd(c, Q, K, V, O, lse, ws, s)) return r;
+    if (!c->merges.empty()) {
+        const dim3 grid((unsigned)c->merges.size(), c->H, kCrossRows / 8);
+        const float *po = ws_ptr<float>(ws, c->ws.part_o), *pl = ws_ptr<float>(ws, c->ws.part_lse);
+        if (c->d == 128) cross_merge_kernel<128><<<grid, 256, 0, s>>>(c->d_merges, po, pl, c->slots, CrossRows(O), lse, c->Lq);
+        else cross_merge_kernel<64><<<grid, 256, 0, s>>>(c->d_merges, po, pl, c->slots, CrossRows(O), lse, c->Lq);
+        MOC_LAUNCH_CHECK();
+    }
+    return MOC_OK;
+}
+
+extern "C" int moc_cross_attend_bwd(const moc_cross *c, const moc_rows *Q, const moc_rows *K, const moc_rows *V, const moc_rows *O,
+                                    const float *lse, const moc_rows *dO, const moc_rows *dQ, const moc_rows *dK, const moc_rows *dV, void *ws,
+                                    void *stream) {
+    moc::NvtxRange nvtx_range("moc_cross_attend_bwd");
+    if (int r = enter_cross(c)) return r;
+    for (const moc_rows *t : {Q, O, dO, dQ}) if (int r = check_rows(t, c->H, c->Lq, c->d, 2)) return r;
+    for (const moc_rows *t : {K, V, dK, dV}) if (int r = check_rows(t, c->Hkv, c->Lk, c->d, 2)) return r;
+    if (c->Lq > 0 && !lse) return MOC_ERR_NULL;
+    if (!aligned(lse, 4)) return MOC_ERR_ALIGN;
+    if (int r = check_ws(ws)) return r;
+    cudaStream_t s = (cudaStream_t)stream;
+    if (c->Lq > 0) {
+        const int64_t rows = (int64_t)c->H * c->Lq, per_block = 8 * 2 * (32 / (c->d / 8));
+        const unsigned grid = (unsigned)std::min<int64_t>((rows + per_block - 1) / per_block, 8ll * c->n_sm);
+        float *delta = ws_ptr<float>(ws, c->ws.delta);
+        int *status = ws_ptr<int>(ws, c->ws.status);
+        if (c->d == 128) cross_delta_kernel<128><<<grid, 256, 0, s>>>(CrossRows(O), CrossRows(dO), delta, status, c->H, c->Lq);
+        else cross_delta_kernel<64><<<grid, 256, 0, s>>>(CrossRows(O), CrossRows(dO), delta, status, c->H, c->Lq);
+        MOC_LAUNCH_CHECK();
+        if (int r = launch_cross_dq(c, Q, K, V, lse, dO, dQ, ws, s)) return r;
+        if (!c->dq_merges.empty()) {
+            const dim3 g2((unsigned)c->dq_merges.size(), c->H, 16);
+            const float *part = ws_ptr<float>(ws, c->ws.part_dq);
+            if (c->d == 128) cross_sum_dq_kernel<128><<<g2, 256, 0, s>>>(c->d_dq_merges, part, c->dq_slots, CrossRows(dQ));
+            else cross_sum_dq_kernel<64><<<g2, 256, 0, s>>>(c->d_dq_merges, part, c->dq_slots, CrossRows(dQ));
+            MOC_LAUNCH_CHECK();
+        }
+        if (!c->pieces.empty())
+            if (int r = launch_cross_dkv(c, Q, K, V, lse, dO, dK, dV, ws, s)) return r;
+    } else {
+        MOC_CUDA_TRY(cudaMemsetAsync(ws_ptr<int>(ws, c->ws.status), 0, 8, s));
+    }
+    if (!c->sums.empty()) {
+        const dim3 g3((unsigned)c->sums.size(), 2, 16);
+        const float *part = ws_ptr<float>(ws, c->ws.part_kv);
+        if (c->d == 128) cross_sum_kv_kernel<128><<<g3, 256, 0, s>>>(c->d_sums, part, CrossRows(dK), CrossRows(dV));
+        else cross_sum_kv_kernel<64><<<g3, 256, 0, s>>>(c->d_sums, part, CrossRows(dK), CrossRows(dV));
+        MOC_LAUNCH_CHECK();
+    }
+    return MOC_OK;
+}
+
+extern "C" int moc_cross_get_status(const moc_cross *c, const void *ws, void *stream, int *device_status, int *detail) {
+    if (int r = enter_cross(c)) return r;
+    if (!device_status) return MOC_ERR_NULL;
+    if (int r = check_ws(ws)) return r;
+    int32_t st[2] = {0, 0};
+    MOC_CUDA_TRY(cudaMemcpyAsync(st, ws_ptr<int32_t>(ws, c->ws.status), sizeof st, cudaMemcpyDeviceToHost, (cudaStream_t)stream));
+    MOC_CUDA_TRY(cudaStreamSynchronize((cudaStream_t)stream));
+    *device_status = st[0];
+    if (detail) *detail = st[1];
+    return MOC_OK;
+}

@@ -1,0 +1,84 @@
+// Cross attention: the plan's tables and what its files share.
+#pragma once
+#include <vector>
+
+#include "moc_common.cuh"
+
+namespace moc {
+
+// A work item of the forward (up to 256 query rows of one segment) or of dQ (up to 128), of every head: its queries, its keys (n_keys
+// may be 0 in the forward), and where its share of the keys goes if there are other shares: the partial slot, -1 for none.
+struct __align__(16) CrossItem { int32_t q0, rows, k0, n_keys, slot, pad[3]; };
+// Rows whose partial results are put together: n slots from `slot` on.
+struct __align__(16) CrossMerge { int32_t q0, rows, slot, n; };
+// A piece of the key-stationary pass: up to 128 keys of a key head against units [u0, u1) of query rows; unit u: query head
+// h * group + u / q_tiles, rows q0 + 128 (u mod q_tiles) of the segment's [q0, q1).
+struct __align__(16) CrossPiece { int32_t h, k0, keys, q0, q1, u0, u1, slot; };
+// Rows of a key head's dK and dV that are sums of n slots (0: zeros).
+struct __align__(16) CrossSum { int32_t h, k0, rows, slot, n, pad[3]; };
+
+constexpr int kCrossRows = 256;
+
+struct CrossLayout {
+    size_t status;
+    size_t part_o, part_lse;       // forward: [H][slots][256][d] and [H][slots][256] fp32
+    size_t fwd_end;
+    size_t delta;                  // [H][Lq]
+    size_t part_dq;                // [H][slots][128][d] fp32
+    size_t part_kv;                // [slots][2][128][d] fp32
+    size_t bwd_end;
+};
+
+}  // namespace moc
+
+struct moc_cross {
+    int H, Hkv, g, d, Lq, Lk, device, n_sm;
+    float scale;
+    std::vector<moc::CrossItem> items, dq_items;       // per head, the longest first
+    std::vector<moc::CrossMerge> merges, dq_merges;    // per head
+    std::vector<moc::CrossPiece> pieces;
+    std::vector<int32_t> piece_off;                    // of every CTA of the key-stationary pass
+    std::vector<moc::CrossSum> sums;
+    int slots = 0, dq_slots = 0, kv_slots = 0;         // per head, per head, in all
+    void *d_blob = nullptr;
+    moc::CrossItem *d_items, *d_dq_items;
+    moc::CrossMerge *d_merges, *d_dq_merges;
+    moc::CrossPiece *d_pieces;
+    int32_t *d_piece_off;
+    moc::CrossSum *d_sums;
+    moc::CrossLayout ws;
+};
+
+namespace moc {
+
+// a caller's rows of bf16 on the device
+struct CrossRows {
+    __nv_bfloat16 *p;
+    int64_t head, tok;
+    CrossRows() = default;
+    explicit CrossRows(const moc_rows *r) : p(static_cast<__nv_bfloat16 *>(r->data)), head(r->head_stride), tok(r->token_stride) {}
+#ifdef __CUDACC__
+    __device__ __forceinline__ __nv_bfloat16 *row(int h, int t) const { return p + h * head + t * tok; }
+#endif
+};
+
+#ifdef __CUDACC__
+// A CTA's n-th item of a list that is sorted by length: every other round in reverse, so that no CTA has the longest of each.
+__device__ __forceinline__ int cross_item(int n) {
+    return n * (int)gridDim.x + ((n & 1) ? (int)gridDim.x - 1 - (int)blockIdx.x : (int)blockIdx.x);
+}
+#endif
+
+int launch_cross_fwd(const moc_cross *c, const moc_rows *Q, const moc_rows *K, const moc_rows *V, const moc_rows *O, float *lse, void *ws,
+                     cudaStream_t s);
+int launch_cross_dq(const moc_cross *c, const moc_rows *Q, const moc_rows *K, const moc_rows *V, const float *lse, const moc_rows *dO,
+                    const moc_rows *dQ, void *ws, cudaStream_t s);
+int launch_cross_dkv(const moc_cross *c, const moc_rows *Q, const moc_rows *K, const moc_rows *V, const float *lse, const moc_rows *dO,
+                     const moc_rows *dK, const moc_rows *dV, void *ws, cudaStream_t s);
+// items: rows of one head's tile list x heads, as one launch of up to `most` CTAs
+static inline unsigned cross_grid(const moc_cross *c, size_t items) {
+    const size_t n = items * (size_t)c->H;
+    return (unsigned)(n < (size_t)c->n_sm ? n : (size_t)c->n_sm);
+}
+
+}  // namespace moc

@@ -95,6 +95,12 @@ __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap *map
                  ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar)
                  : "memory");
 }
+// the same of a 3-D tensor (columns, rows, heads)
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap *map, int x, int y, int z, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+                 : "memory");
+}
 // four rows of a 2-D tensor, 64 columns from column x on, into four consecutive 128-byte rows of shared memory
 __device__ __forceinline__ void tma_gather4(uint32_t dst, const CUtensorMap *map, int x, int r0, int r1, int r2, int r3, uint32_t bar) {
     asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.tile::gather4.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];"
@@ -344,5 +350,7 @@ __device__ __forceinline__ void store_quad(__nv_bfloat16 *row, int i, const uint
 
 // host: encode a 2-D bf16 tensor map [rows][cols], box {64 cols, box_rows}, 128-byte swizzle
 int make_tmap_2d_bf16(CUtensorMap *map, const void *base, uint64_t rows, uint64_t cols, uint32_t box_rows);
+// host: the same of a caller's rows [heads][rows][cols] of any strides, box {64 cols, box_rows, 1}
+int make_tmap_rows_bf16(CUtensorMap *map, const moc_rows *r, uint64_t heads, uint64_t rows, uint64_t cols, uint32_t box_rows);
 
 }  // namespace moc
