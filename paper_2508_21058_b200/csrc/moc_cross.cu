@@ -143,42 +143,6 @@ static void derive_cross(moc_cross *c, const moc_cross_problem *pr) {
     w.bwd_end = up256(w.part_kv + 4 * 2 * (size_t)c->kv_slots * 128 * d);
 }
 
-// ---- delta_i = sum_x dO_ix O_ix, a warp a row pair: 16 lanes a row at d = 128, 8 at d = 64, 16 bytes a lane
-template <int D>
-__global__ void __launch_bounds__(256) cross_delta_kernel(CrossRows O, CrossRows dO, float *delta, int *status, int H, int Lq) {
-    constexpr int LPR = D / 8, RPW = 32 / LPR, U = 2;
-    if (blockIdx.x == 0 && threadIdx.x == 0) status[ST_STATUS] = status[ST_DETAIL] = 0;
-    const int lane = threadIdx.x & 31, chunk = lane % LPR;
-    const int64_t n = (int64_t)H * Lq;
-    for (int64_t r0 = ((int64_t)blockIdx.x * 8 + (threadIdx.x >> 5)) * (U * RPW); r0 < n; r0 += (int64_t)gridDim.x * 8 * (U * RPW)) {
-        uint4 a[U], b[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int64_t r = r0 + u * RPW + lane / LPR;
-            a[u] = b[u] = make_uint4(0, 0, 0, 0);
-            if (r < n) {
-                const int h = (int)(r / Lq), t = (int)(r - (int64_t)h * Lq);
-                a[u] = *reinterpret_cast<const uint4 *>(O.row(h, t) + chunk * 8);
-                b[u] = *reinterpret_cast<const uint4 *>(dO.row(h, t) + chunk * 8);
-            }
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int64_t r = r0 + u * RPW + lane / LPR;
-            const uint32_t x[4] = {a[u].x, a[u].y, a[u].z, a[u].w}, y[4] = {b[u].x, b[u].y, b[u].z, b[u].w};
-            float v = 0.f;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                v = fmaf(__uint_as_float(x[i] << 16), __uint_as_float(y[i] << 16), v);
-                v = fmaf(__uint_as_float(x[i] & 0xffff0000u), __uint_as_float(y[i] & 0xffff0000u), v);
-            }
-#pragma unroll
-            for (int o = LPR / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-            if (r < n && chunk == 0) delta[r] = v;
-        }
-    }
-}
-
 // ---- shares of the forward: O = sum_i w_i O_i / sum_i w_i, w_i = exp(lse_i - max lse); a warp a row
 template <int D>
 __global__ void __launch_bounds__(256) cross_merge_kernel(const CrossMerge *merges, const float *part_o, const float *part_lse, int slots,
@@ -362,14 +326,7 @@ extern "C" int moc_cross_attend_bwd(const moc_cross *c, const moc_rows *Q, const
     if (int r = check_ws(ws)) return r;
     cudaStream_t s = (cudaStream_t)stream;
     if (c->Lq > 0) {
-        const int64_t rows = (int64_t)c->H * c->Lq, per_block = 8 * 2 * (32 / (c->d / 8));
-        const unsigned grid = (unsigned)std::min<int64_t>((rows + per_block - 1) / per_block, 8ll * c->n_sm);
-        float *delta = ws_ptr<float>(ws, c->ws.delta);
-        int *status = ws_ptr<int>(ws, c->ws.status);
-        if (c->d == 128) cross_delta_kernel<128><<<grid, 256, 0, s>>>(CrossRows(O), CrossRows(dO), delta, status, c->H, c->Lq);
-        else cross_delta_kernel<64><<<grid, 256, 0, s>>>(CrossRows(O), CrossRows(dO), delta, status, c->H, c->Lq);
-        MOC_LAUNCH_CHECK();
-        if (int r = launch_cross_dq(c, Q, K, V, lse, dO, dQ, ws, s)) return r;
+        if (int r = launch_cross_dq(c, Q, K, V, O, lse, dO, dQ, ws, s)) return r;
         if (!c->dq_merges.empty()) {
             const dim3 g2((unsigned)c->dq_merges.size(), c->H, 16);
             const float *part = ws_ptr<float>(ws, c->ws.part_dq);

@@ -71,7 +71,8 @@ __device__ __forceinline__ int cross_item(int n) {
 
 int launch_cross_fwd(const moc_cross *c, const moc_rows *Q, const moc_rows *K, const moc_rows *V, const moc_rows *O, float *lse, void *ws,
                      cudaStream_t s);
-int launch_cross_dq(const moc_cross *c, const moc_rows *Q, const moc_rows *K, const moc_rows *V, const float *lse, const moc_rows *dO,
+// (also writes delta)
+int launch_cross_dq(const moc_cross *c, const moc_rows *Q, const moc_rows *K, const moc_rows *V, const moc_rows *O, const float *lse, const moc_rows *dO,
                     const moc_rows *dQ, void *ws, cudaStream_t s);
 int launch_cross_dkv(const moc_cross *c, const moc_rows *Q, const moc_rows *K, const moc_rows *V, const float *lse, const moc_rows *dO,
                      const moc_rows *dK, const moc_rows *dV, void *ws, cudaStream_t s);

@@ -11,10 +11,10 @@
 //               keeps its 64 P values between T1 and T2;
 //   warp 8      K and V tiles (three and two stages, running across items).  A segment's last tile comes in boxes of 16 rows, and the one
 //               its end lies in row by row with zeros behind it: K is summed over, and of V's rows dP must be a number;
-//   warp 9      the next item's Q and dO tiles, its lse and delta;
+//   warp 9      the next item's Q and dO tiles and its lse;
+//   warps 10, 11, 14, 15  its delta, 32 rows each;
 //   warps 12,13 MMA issuers: warp 12 T1, warp 13 T2 and ACC.  T1(j + 1) is issued once the lanes have read T1(j), T2(j + 2)
-//               after ACC(j), which reads the dS over T2(j);
-//   warps 10, 11, 14, 15 idle (they complete the warpgroups; the lanes take the registers the others give up).
+//               after ACC(j), which reads the dS over T2(j).
 #include <algorithm>
 
 #include "moc_cross.cuh"
@@ -27,8 +27,9 @@ using namespace tc;
 struct CrossDqParams {
     const CrossItem *items;
     int n_all, H, g, Lq, slots;
-    CrossRows K, V, dQ;
-    const float *lse, *delta;
+    CrossRows K, V, O, dO, dQ;
+    const float *lse;
+    float *delta;                 // [H][Lq], written here for dK and dV
     float *part;                  // [H][slots][128][D] shares of dQ
     int *status;
     float scale, scale_log2;
@@ -37,6 +38,7 @@ struct CrossDqParams {
 
 enum CrossDqWait { CQ_XFULL = 96, CQ_XEMPTY, CQ_YFULL, CQ_YEMPTY, CQ_T1FULL, CQ_T2FULL, CQ_READ, CQ_DSDONE, CQ_ACCFULL, CQ_ACCFREE, CQ_SMEM };
 
+constexpr int kDeltaWarps = 4;    // each forms delta of 32 rows of an item
 constexpr int kCrossDqThreads = 512, kCrossKStages = 3, kCrossVStages = 2;
 
 template <int D>
@@ -69,7 +71,9 @@ __global__ void __launch_bounds__(kCrossDqThreads, 1) cross_dq_tc_kernel(const _
     }
     if (threadIdx.x == 0) {
         s_abort = 0;
-        mbar_init(bar(X_FULL), 2);                          // the tiles' bytes; lse and delta
+        // (a wait runs out a second after the launch at the earliest)
+        if (blockIdx.x == 0) p.status[ST_STATUS] = p.status[ST_DETAIL] = 0;
+        mbar_init(bar(X_FULL), 2 + kDeltaWarps);            // the tiles' bytes; lse; delta
         mbar_init(bar(X_EMPTY), 2 + 8);                     // both issuers, and each lane warp when it has the item's data
         for (int t = 0; t < kCrossKStages; ++t) { mbar_init(bar(K_FULL + t), 2); mbar_init(bar(K_EMPTY + t), 1); }
         for (int t = 0; t < kCrossVStages; ++t) { mbar_init(bar(V_FULL + t), 2); mbar_init(bar(V_EMPTY + t), 1); }
@@ -91,6 +95,72 @@ __global__ void __launch_bounds__(kCrossDqThreads, 1) cross_dq_tc_kernel(const _
     // TMEM columns: T1 [0,128)  T2 of the even tiles [128,256)  ACC [256,384)  T2 of the odd tiles [384,512)
     const uint32_t tmem = tmem_slot;
     volatile int *abort_flag = &s_abort;
+
+    // delta_i = sum_x dO_ix O_ix of rows 32 dw .. 32 dw + 31 of every item, formed while the item before it is in work (the rows are asked
+    // for an item ahead of that): a pass over dO and O less than by a launch of its own, and O is read under the products
+    auto form_delta = [&](int dw) __attribute__((always_inline)) {
+        constexpr int CH = D / 8, RP = 32 / CH, B = 4;         // lanes a row, rows an instruction, instructions under way
+        const int sub = lane / CH, c16 = lane % CH;
+        int n_x = 0;
+        bool ok = true;
+        for (int n = 0; ok; ++n) {
+            const int id = cross_item(n);
+            if (n * (int)gridDim.x >= p.n_all) break;
+            if (id >= p.n_all) continue;
+            const int rank = id / p.H, h = id - rank * p.H;
+            const CrossItem it = p.items[rank];
+            if (it.n_keys == 0) continue;
+            const int next = cross_item(n + 1);
+            if (next < p.n_all) {
+                const int nr = next / p.H, nh = next - nr * p.H;
+                const int q = p.items[nr].q0 + dw * 32 + lane;
+                if (dw * 32 + lane < p.items[nr].rows)
+#pragma unroll
+                    for (int x = 0; x < D / 64; ++x) {
+                        asm volatile("prefetch.global.L2 [%0];" ::"l"(p.O.row(nh, q) + x * 64));
+                        asm volatile("prefetch.global.L2 [%0];" ::"l"(p.dO.row(nh, q) + x * 64));
+                    }
+            }
+            float mine = 0.f;
+#pragma unroll 1
+            for (int r0 = 0; r0 < 32; r0 += B * RP) {
+                uint4 a[B], b[B];
+#pragma unroll
+                for (int y = 0; y < B; ++y) {
+                    const int r = dw * 32 + r0 + y * RP + sub;
+                    a[y] = b[y] = make_uint4(0, 0, 0, 0);
+                    if (r < it.rows) {
+                        a[y] = *reinterpret_cast<const uint4 *>(p.O.row(h, it.q0 + r) + c16 * 8);
+                        b[y] = *reinterpret_cast<const uint4 *>(p.dO.row(h, it.q0 + r) + c16 * 8);
+                    }
+                }
+#pragma unroll
+                for (int y = 0; y < B; ++y) {
+                    const uint32_t u[4] = {a[y].x, a[y].y, a[y].z, a[y].w}, w[4] = {b[y].x, b[y].y, b[y].z, b[y].w};
+                    float v = 0.f;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        v = fmaf(__uint_as_float(u[i] << 16), __uint_as_float(w[i] << 16), v);
+                        v = fmaf(__uint_as_float(u[i] & 0xffff0000u), __uint_as_float(w[i] & 0xffff0000u), v);
+                    }
+#pragma unroll
+                    for (int o = CH / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+                    // lane l keeps row l of the 32
+                    v = __shfl_sync(0xffffffffu, v, (lane % RP) * CH);
+                    if (lane / RP == r0 / RP + y) mine = v;
+                }
+            }
+            if (dw * 32 + lane < it.rows) p.delta[(size_t)h * p.Lq + it.q0 + dw * 32 + lane] = mine;
+            if (n_x > 0) {
+                ok = __all_sync(0xffffffffu, mbar_wait(bar(X_EMPTY), (n_x - 1) & 1, abort_flag, p.wait, CQ_XEMPTY));
+                if (!ok) break;
+            }
+            s_ld[n_x & 1][1][dw * 32 + lane] = -mine;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(X_FULL));
+            ++n_x;
+        }
+    };
 
     if (warp < 8) {
         // ------------------------------------------------------------ lane threads
@@ -271,8 +341,10 @@ __global__ void __launch_bounds__(kCrossDqThreads, 1) cross_dq_tc_kernel(const _
         }
     } else if (warp < 12) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
-        // ------------------------------------------------------------ the items' Q and dO, lse and delta (looked up before the buffers are free)
-        if (warp == 9) {
+        // ------------------------------------------------------------ the items' Q and dO and lse (looked up before the buffers are free)
+        if (warp > 9) {
+            form_delta(warp - 10);
+        } else {
             if (lane == 0) { prefetch_tensormap(&tmQ); prefetch_tensormap(&tmdO); }
             int n_x = 0;
             bool ok = true;
@@ -283,16 +355,11 @@ __global__ void __launch_bounds__(kCrossDqThreads, 1) cross_dq_tc_kernel(const _
                 const int rank = id / p.H, h = id - rank * p.H;
                 const CrossItem it = p.items[rank];
                 if (it.n_keys == 0) continue;
-                float l[4], d[4];
+                float l[4];
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
                     const int r = x * 32 + lane;
-                    l[x] = INFINITY;                         // rows that are not there: P = 0
-                    d[x] = 0.f;
-                    if (r < it.rows) {
-                        l[x] = p.lse[(size_t)h * p.Lq + it.q0 + r];
-                        d[x] = p.delta[(size_t)h * p.Lq + it.q0 + r];
-                    }
+                    l[x] = r < it.rows ? p.lse[(size_t)h * p.Lq + it.q0 + r] : INFINITY;       // rows that are not there: P = 0
                 }
                 if (n_x > 0) {
                     ok = __all_sync(0xffffffffu, mbar_wait(bar(X_EMPTY), (n_x - 1) & 1, abort_flag, p.wait, CQ_XEMPTY));
@@ -307,10 +374,7 @@ __global__ void __launch_bounds__(kCrossDqThreads, 1) cross_dq_tc_kernel(const _
                     }
                 }
 #pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    s_ld[n_x & 1][0][x * 32 + lane] = l[x] * -1.4426950408889634f;
-                    s_ld[n_x & 1][1][x * 32 + lane] = -d[x];
-                }
+                for (int x = 0; x < 4; ++x) s_ld[n_x & 1][0][x * 32 + lane] = l[x] * -1.4426950408889634f;
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(X_FULL));
                 ++n_x;
@@ -323,7 +387,9 @@ __global__ void __launch_bounds__(kCrossDqThreads, 1) cross_dq_tc_kernel(const _
     } else {
         // ------------------------------------------------------------ MMA issuers (a warp stays together, one lane of it issues)
         asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
-        if (warp <= 13) {
+        if (warp > 13) {
+            form_delta(warp - 12);
+        } else {
             constexpr uint32_t IDESC_ACC = idesc_bf16_f32(128, D, 0, 1);      // ACC += dS K, K MN-major
             constexpr uint32_t STAGE = TILE_BYTES >> 4;
             auto lo = [](uint64_t d) { return (uint32_t)d; };
@@ -408,7 +474,7 @@ __global__ void __launch_bounds__(kCrossDqThreads, 1) cross_dq_tc_kernel(const _
 }
 
 template <int D>
-static int cross_dq_d(const moc_cross *c, const moc_rows *Q, const moc_rows *K, const moc_rows *V, const float *lse, const moc_rows *dO,
+static int cross_dq_d(const moc_cross *c, const moc_rows *Q, const moc_rows *K, const moc_rows *V, const moc_rows *O, const float *lse, const moc_rows *dO,
                       const moc_rows *dQ, void *ws, cudaStream_t s) {
     CUtensorMap tmQ = {}, tmdO = {}, tmK = {}, tmV = {}, tmK16 = {}, tmV16 = {};
     if (int r = make_tmap_rows_bf16(&tmQ, Q, c->H, c->Lq, D, 128)) return r;
@@ -422,7 +488,7 @@ static int cross_dq_d(const moc_cross *c, const moc_rows *Q, const moc_rows *K, 
     CrossDqParams a;
     a.items = c->d_dq_items; a.n_all = (int)c->dq_items.size() * c->H;
     a.H = c->H; a.g = c->g; a.Lq = c->Lq; a.slots = c->dq_slots;
-    a.K = CrossRows(K); a.V = CrossRows(V); a.dQ = CrossRows(dQ);
+    a.K = CrossRows(K); a.V = CrossRows(V); a.O = CrossRows(O); a.dO = CrossRows(dO); a.dQ = CrossRows(dQ);
     a.lse = lse; a.delta = ws_ptr<float>(ws, c->ws.delta);
     a.part = ws_ptr<float>(ws, c->ws.part_dq);
     a.status = ws_ptr<int>(ws, c->ws.status);
@@ -442,9 +508,9 @@ static int cross_dq_d(const moc_cross *c, const moc_rows *Q, const moc_rows *K, 
     return MOC_OK;
 }
 
-int launch_cross_dq(const moc_cross *c, const moc_rows *Q, const moc_rows *K, const moc_rows *V, const float *lse, const moc_rows *dO,
+int launch_cross_dq(const moc_cross *c, const moc_rows *Q, const moc_rows *K, const moc_rows *V, const moc_rows *O, const float *lse, const moc_rows *dO,
                     const moc_rows *dQ, void *ws, cudaStream_t s) {
-    return c->d == 128 ? cross_dq_d<128>(c, Q, K, V, lse, dO, dQ, ws, s) : cross_dq_d<64>(c, Q, K, V, lse, dO, dQ, ws, s);
+    return c->d == 128 ? cross_dq_d<128>(c, Q, K, V, O, lse, dO, dQ, ws, s) : cross_dq_d<64>(c, Q, K, V, O, lse, dO, dQ, ws, s);
 }
 
 }  // namespace moc
