@@ -276,16 +276,17 @@ class MocPlan:
 
 def _rows(t, heads, tokens, d, dtype, name):
     """A [heads][tokens][d] tensor of any strides as the library takes it."""
-    if t.dtype != dtype or t.dim() != 3 or t.shape[0] != heads or t.shape[1] != tokens or t.shape[2] != d:
+    if t.dtype is not dtype or t.shape != (heads, tokens, d):
         raise MocError(-2, f"moc error -2: {name} is {t.dtype} {tuple(t.shape)}, not {dtype} {(heads, tokens, d)}")
-    if t.stride(2) != 1:
+    head, tok, one = t.stride()
+    if one != 1:
         raise MocError(-2, f"moc error -2: the channels of {name} are not consecutive")
     _on_current(t, name)
-    return _Rows(t.data_ptr(), t.stride(0), t.stride(1))
+    return _Rows(t.data_ptr(), head, tok)
 
 
 def _on_current(t, name):
-    if not t.is_cuda or t.device.index != torch._C._cuda_getDevice():
+    if t.get_device() != torch._C._cuda_getDevice():           # (-1 on the CPU)
         raise MocError(-6, f"moc error -6: {name} is on {t.device}, which is not the current device")
 
 
@@ -293,7 +294,7 @@ def _table(t, shape, dtype, name):
     """The address of a contiguous tensor, or NULL."""
     if t is None:
         return None
-    if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous():
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
         raise MocError(-2, f"moc error -2: {name} is {t.dtype} {tuple(t.shape)}, not contiguous {dtype} {shape}")
     _on_current(t, name)
     return t.data_ptr()

@@ -90,46 +90,63 @@ static void derive_cross(moc_cross *c, const moc_cross_problem *pr) {
     cut_items(c->items, c->merges, c->slots, share_tiles(c->items, c->H, c->n_sm, 128));
     cut_items(c->dq_items, c->dq_merges, c->dq_slots, share_tiles(c->dq_items, c->H, c->n_sm, 0));
 
-    // Key-stationary pass: all (key tile, query tile) pairs in a row, cut into equal stretches, one for every CTA (of two pairs at
-    // least); a key tile that lies in several stretches is a sum of slots.
-    struct Tile { int h, k0, keys, q0, q1; int64_t units; };
-    std::vector<Tile> tiles;
-    int64_t total = 0;
+    // Key-stationary pass.  The query tiles of a (key head, segment) are cut into parts of about the same length, and every key tile of
+    // the segment against one part is a piece; a key tile with several parts is a sum of slots.  Pieces of the same part follow one another, so
+    // that CTAs that run side by side stream the same queries, out of L2 (stretches of all pairs in a row, each CTA at another place
+    // of the stream: 33k queries, 512 states, 24 heads 340 us, of 4.8 TB/s from DRAM).
+    struct Group { int h, s; int64_t units; int n; };                // pairs of a key tile; pieces of a part
+    std::vector<Group> groups;
+    int64_t total = 0, longest = 0;
     for (int h = 0; h < c->Hkv; ++h)
         for (int s = 0; s < S; ++s) {
             const int64_t units = (int64_t)c->g * ((pr->q_off[s + 1] - pr->q_off[s] + 127) / 128);
-            const int end = pr->k_off[s] + keys(s);
-            for (int k = pr->k_off[s]; k < pr->k_off[s + 1];) {
-                const int n = std::min(128, (k < end ? end : pr->k_off[s + 1]) - k);
-                if (k >= end || units == 0) c->sums.push_back(CrossSum{h, k, n, 0, 0, {}});
-                else { tiles.push_back(Tile{h, k, n, pr->q_off[s], pr->q_off[s + 1], units}); total += units; }
-                k += n;
-            }
+            const int nk = units == 0 ? 0 : keys(s);                 // states that somebody reads
+            if (nk > 0) groups.push_back(Group{h, s, units, (nk + 127) / 128});
+            total += units * ((nk + 127) / 128);
+            if (nk > 0) longest = std::max(longest, units);
+            for (int k = pr->k_off[s] + nk; k < pr->k_off[s + 1]; k += 128)
+                c->sums.push_back(CrossSum{h, k, std::min(128, pr->k_off[s + 1] - k), 0, 0, {}});
         }
-    const int64_t n_cta = std::min<int64_t>(c->n_sm, (total + 1) / 2);
-    size_t ti = 0;
-    int64_t base = 0;                                    // units before tile ti
+    std::stable_sort(groups.begin(), groups.end(), [](const Group &a, const Group &b) { return a.units > b.units; });
+    // The length of a part with the least estimated time: rounds of n_sm pieces, each as long as its first, where a piece costs two pairs
+    // beside its own (its key tile, its results, the launch that adds them up).
+    int64_t part = std::max<int64_t>(longest, 1);
+    double best = 1e300;
+    for (int64_t n = 1; n <= std::min<int64_t>(longest, 256); ++n) {
+        const int64_t len = (longest + n - 1) / n;
+        double t = 0;
+        int64_t at = 0;                                              // pieces so far
+        for (const Group &g : groups) {
+            const int64_t parts = (g.units + len - 1) / len, end = at + parts * g.n;
+            // rounds that begin in this group
+            t += (double)((end + c->n_sm - 1) / c->n_sm - (at + c->n_sm - 1) / c->n_sm) * (2.0 + (double)g.units / parts);
+            at = end;
+        }
+        if (t < best) { best = t; part = len; }
+        if (at > 64ll * c->n_sm) break;                              // (shorter parts only cost more)
+    }
+    std::vector<CrossPiece> all;
+    for (const Group &g : groups) {
+        const int64_t parts = (g.units + part - 1) / part;
+        const int s = g.s, slot0 = c->kv_slots;
+        for (int64_t x = 0; x < parts; ++x)
+            for (int kt = 0; kt < g.n; ++kt) {
+                const int k0 = pr->k_off[s] + kt * 128, rows = std::min(128, keys(s) - kt * 128);
+                all.push_back(CrossPiece{g.h, k0, rows, pr->q_off[s], pr->q_off[s + 1], (int)(g.units * x / parts), (int)(g.units * (x + 1) / parts),
+                                         parts > 1 ? slot0 + (int)(kt * parts + x) : -1});
+                if (x == 0 && parts > 1) c->sums.push_back(CrossSum{g.h, k0, rows, slot0 + (int)(kt * parts), (int)parts, {}});
+            }
+        if (parts > 1) c->kv_slots += (int)(parts * g.n);
+    }
+    // dealt to the CTAs in turn, every other round in reverse
+    const int64_t n_cta = std::min<int64_t>(c->n_sm, (int64_t)all.size());
     c->piece_off.push_back(0);
     for (int64_t b = 0; b < n_cta; ++b) {
-        int64_t at = total * b / n_cta;
-        const int64_t end = total * (b + 1) / n_cta;
-        while (at < end) {
-            const Tile &t = tiles[ti];
-            const int64_t upto = std::min(end, base + t.units);
-            c->pieces.push_back(CrossPiece{t.h, t.k0, t.keys, t.q0, t.q1, (int)(at - base), (int)(upto - base), -1});
-            at = upto;
-            if (at == base + t.units) { base += t.units; ++ti; }
+        for (int64_t r = 0; r * n_cta < (int64_t)all.size(); ++r) {
+            const int64_t i = r * n_cta + ((r & 1) ? n_cta - 1 - b : b);
+            if (i < (int64_t)all.size()) c->pieces.push_back(all[i]);
         }
         c->piece_off.push_back((int)c->pieces.size());
-    }
-    for (size_t a = 0; a < c->pieces.size();) {
-        size_t e = a + 1;
-        while (e < c->pieces.size() && c->pieces[e].u0 != 0) ++e;
-        if (e - a > 1) {
-            c->sums.push_back(CrossSum{c->pieces[a].h, c->pieces[a].k0, c->pieces[a].keys, c->kv_slots, (int)(e - a), {}});
-            for (size_t x = a; x < e; ++x) c->pieces[x].slot = c->kv_slots++;
-        }
-        a = e;
     }
     CrossLayout &w = c->ws;
     const size_t H = c->H, d = c->d;
@@ -175,35 +192,32 @@ __global__ void __launch_bounds__(256) cross_merge_kernel(const CrossMerge *merg
     if (lane == 0) lse[(size_t)h * Lq + m.q0 + row] = big + __logf(sum);
 }
 
-// ---- shares of a gradient: out = sum of the slots, in their order; a warp a row
+// ---- shares of a gradient: out = sum of the slots, in their order; 16 bytes a lane, so a warp has one row at d = 128, two at 64
 template <int D>
 __device__ __forceinline__ void sum_row(const float *src, size_t stride, int n, __nv_bfloat16 *dst) {
-    constexpr int V = D / 32;
-    float acc[V] = {};
-    for (int i = 0; i < n; ++i)
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i = 0; i < n; i += 4) {
+        float4 v[4];
 #pragma unroll
-        for (int x = 0; x < V; x += 2) {
-            const float2 v = *reinterpret_cast<const float2 *>(src + i * stride + x);
-            acc[x] += v.x;
-            acc[x + 1] += v.y;
-        }
+        for (int x = 0; x < 4; ++x) v[x] = i + x < n ? *reinterpret_cast<const float4 *>(src + (i + x) * stride) : make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-    for (int x = 0; x < V; x += 2) reinterpret_cast<uint32_t *>(dst)[x / 2] = tc::bf16x2(acc[x], acc[x + 1]);
+        for (int x = 0; x < 4; ++x) { acc.x += v[x].x; acc.y += v[x].y; acc.z += v[x].z; acc.w += v[x].w; }
+    }
+    *reinterpret_cast<uint2 *>(dst) = make_uint2(tc::bf16x2(acc.x, acc.y), tc::bf16x2(acc.z, acc.w));
 }
 template <int D>
 __global__ void __launch_bounds__(256) cross_sum_dq_kernel(const CrossMerge *merges, const float *part, int slots, CrossRows dQ) {
     const CrossMerge m = merges[blockIdx.x];
-    const int h = blockIdx.y, row = blockIdx.z * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    const int h = blockIdx.y, at = (blockIdx.z * 256 + threadIdx.x) * 4, row = at / D, col = at % D;
     if (row < m.rows)
-        sum_row<D>(part + (((size_t)h * slots + m.slot) * 128 + row) * D + lane * (D / 32), (size_t)128 * D, m.n, dQ.row(h, m.q0 + row) + lane * (D / 32));
+        sum_row<D>(part + (((size_t)h * slots + m.slot) * 128 + row) * D + col, (size_t)128 * D, m.n, dQ.row(h, m.q0 + row) + col);
 }
 template <int D>
 __global__ void __launch_bounds__(256) cross_sum_kv_kernel(const CrossSum *sums, const float *part, CrossRows dK, CrossRows dV) {
     const CrossSum m = sums[blockIdx.x];
-    const int side = blockIdx.y, row = blockIdx.z * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    const int side = blockIdx.y, at = (blockIdx.z * 256 + threadIdx.x) * 4, row = at / D, col = at % D;
     if (row < m.rows)
-        sum_row<D>(part + (((size_t)m.slot * 2 + side) * 128 + row) * D + lane * (D / 32), (size_t)2 * 128 * D, m.n,
-                   (side ? dV : dK).row(m.h, m.k0 + row) + lane * (D / 32));
+        sum_row<D>(part + (((size_t)m.slot * 2 + side) * 128 + row) * D + col, (size_t)2 * 128 * D, m.n, (side ? dV : dK).row(m.h, m.k0 + row) + col);
 }
 
 static int enter_cross(const moc_cross *c) {
@@ -328,7 +342,7 @@ extern "C" int moc_cross_attend_bwd(const moc_cross *c, const moc_rows *Q, const
     if (c->Lq > 0) {
         if (int r = launch_cross_dq(c, Q, K, V, O, lse, dO, dQ, ws, s)) return r;
         if (!c->dq_merges.empty()) {
-            const dim3 g2((unsigned)c->dq_merges.size(), c->H, 16);
+            const dim3 g2((unsigned)c->dq_merges.size(), c->H, c->d / 8);      // 1024 values a block
             const float *part = ws_ptr<float>(ws, c->ws.part_dq);
             if (c->d == 128) cross_sum_dq_kernel<128><<<g2, 256, 0, s>>>(c->d_dq_merges, part, c->dq_slots, CrossRows(dQ));
             else cross_sum_dq_kernel<64><<<g2, 256, 0, s>>>(c->d_dq_merges, part, c->dq_slots, CrossRows(dQ));
@@ -340,7 +354,7 @@ extern "C" int moc_cross_attend_bwd(const moc_cross *c, const moc_rows *Q, const
         MOC_CUDA_TRY(cudaMemsetAsync(ws_ptr<int>(ws, c->ws.status), 0, 8, s));
     }
     if (!c->sums.empty()) {
-        const dim3 g3((unsigned)c->sums.size(), 2, 16);
+        const dim3 g3((unsigned)c->sums.size(), 2, c->d / 8);
         const float *part = ws_ptr<float>(ws, c->ws.part_kv);
         if (c->d == 128) cross_sum_kv_kernel<128><<<g3, 256, 0, s>>>(c->d_sums, part, CrossRows(dK), CrossRows(dV));
         else cross_sum_kv_kernel<64><<<g3, 256, 0, s>>>(c->d_sums, part, CrossRows(dK), CrossRows(dV));

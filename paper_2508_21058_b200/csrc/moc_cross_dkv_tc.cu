@@ -98,8 +98,7 @@ __global__ void __launch_bounds__(kCrossKvThreads, 1) cross_dkv_tc_kernel(const 
         int s3 = 0, ph3 = 0, jt = 0;                  // Y1 stage of tile jt and its phase; tiles of all pieces
         bool t1_early = false, y1_early = false;      // barriers looked at ahead of their waits
         for (int pi = piece0; ok && pi < piece1; ++pi) {
-            const CrossPiece pc = p.pieces[pi];
-            for (const int end = jt + pc.u1 - pc.u0; jt < end; ++jt) {
+            for (const int end = jt + p.pieces[pi].u1 - p.pieces[pi].u0; jt < end; ++jt) {
                 const int st = jt & 1;
                 ok = t1_early || mbar_wait_spin(bar(T1_FULL + st), (jt >> 1) & 1, abort_flag, p.wait, CB_T1FULL);
                 ok = ok && (y1_early || mbar_wait(bar(Y1_FULL + s3), ph3, abort_flag, p.wait, CB_YFULL));
@@ -178,6 +177,7 @@ __global__ void __launch_bounds__(kCrossKvThreads, 1) cross_dkv_tc_kernel(const 
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
             tc_fence_after();
+            const CrossPiece pc = p.pieces[pi];              // (read here: kept from before the loop, it would take the loop's registers)
             constexpr int NJ = D / 32;                       // groups of eight rows that this warp has
             const int l4 = lane >> 2, l2 = lane & 3, cb = D == 128 ? half : 0, j0 = D == 128 ? 0 : 2 * half;
 #pragma unroll 1

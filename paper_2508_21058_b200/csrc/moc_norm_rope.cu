@@ -5,16 +5,20 @@
 //   Backward:  g = the rotation by -t of dy,  xh = x r,  dw = sum over heads and tokens of g xh,
 //   dx = r (w g - xh mean_c(w g xh)).
 //
-// Both are bound by HBM: each value is read once and written once, and what a row needs beside its own values is shared by all
-// heads of a token.  So a warp takes a token and walks its heads: the angles - formed in turns, in 64 bits, reduced to a part of a
-// turn and only then rounded to 32, so that far positions lose nothing - are made once for all of them.  A lane holds eight consecutive channels
-// (16 bytes of bf16), 16 lanes a row at d = 128 and 8 at d = 64; four rows a lane are under way at a time.
+// Both are bound by HBM where instructions do not get in the way: each value is read once and written once, and what a row needs
+// beside its own values is shared by all heads of a token.  So a warp takes a token and walks its heads: the angles - formed in turns, in 64
+// bits, reduced to a part of a turn and only then rounded to 32, so that far positions lose nothing - are made once for all of them.
+// A lane holds four pairs of channels of a row (16 lanes a row at d = 128, 8 at d = 64), the first channels of two pairs in one packed register and
+// the second ones in another, whichever channels the pairs are of: the norm, the rotation and their gradients are packed multiply-adds, and the
+// rotation needs no other lane.
 // Where there are too few tokens to fill the GPU, a token's heads are dealt to several warps.
 #include <algorithm>
 #include <math.h>
 #include <new>
+#include <type_traits>
 
 #include "moc_common.cuh"
+#include "moc_tc.cuh"
 
 namespace moc {
 
@@ -38,7 +42,6 @@ struct moc_rope {
 namespace moc {
 
 constexpr int kRopeWarps = 8;         // warps per block, each with a token of its own
-constexpr int kRopeBlocksPerSm = 3;
 
 // one of the two tensors of a call
 struct RopeSide {
@@ -60,88 +63,142 @@ struct RopeParams {
     float eps, inv_d;
 };
 
-// eight consecutive values as fp32
-template <typename T> struct Raw8;
-template <> struct Raw8<__nv_bfloat16> {
-    uint4 a;
-    __device__ __forceinline__ void load(const __nv_bfloat16 *p) { a = *reinterpret_cast<const uint4 *>(p); }
-    __device__ __forceinline__ void zero() { a = make_uint4(0, 0, 0, 0); }
-    __device__ __forceinline__ void get(float (&v)[8]) const {
-        const uint32_t u[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            v[2 * i] = __uint_as_float(u[i] << 16);
-            v[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+using tc::add2;
+using tc::fma2;
+using tc::mul2;
+using tc::pack2;
+using tc::unpack2;
+
+// A lane's four pairs: a[k] the first channels of pairs 2 k and 2 k + 1, b[k] the second ones.
+struct Pairs {
+    uint64_t a[2], b[2];
+};
+__device__ __forceinline__ uint64_t both(float v) { return pack2(v, v); }
+
+// The channels of a lane's pairs.  Neighbours: eight consecutive ones.  Halves: lanes up to n_pairs / 4 have four channels and the four that
+// are n_pairs behind them, the others eight that are not turned.  `lo`, `hi`: where its two blocks of four begin.
+struct Channels {
+    int lo, hi;
+    __device__ __forceinline__ Channels(bool halves, int chunk, int n_pairs) {
+        const int turned = n_pairs >> 2;
+        lo = !halves ? chunk * 8 : chunk < turned ? chunk * 4 : 2 * n_pairs + (chunk - turned) * 8;
+        hi = halves && chunk < turned ? n_pairs + chunk * 4 : lo + 4;
+    }
+    // channel of place i (0..3) among the first (second = 0) or second channels
+    __device__ __forceinline__ int of(bool halves, int i, int second) const {
+        if (halves) return (second ? hi : lo) + i;
+        return lo + 2 * i + second;
+    }
+};
+
+// a lane's part of a row, as it is loaded: its two blocks of four channels
+template <typename T> struct Raw;
+template <> struct Raw<__nv_bfloat16> {
+    uint4 u;
+    template <bool HALVES>
+    __device__ __forceinline__ void load(const __nv_bfloat16 *row, const Channels &c) {
+        if (HALVES) {
+            const uint2 x = *reinterpret_cast<const uint2 *>(row + c.lo), y = *reinterpret_cast<const uint2 *>(row + c.hi);
+            u = make_uint4(x.x, x.y, y.x, y.y);
+        } else {
+            u = *reinterpret_cast<const uint4 *>(row + c.lo);
         }
     }
-};
-template <> struct Raw8<float> {
-    float4 a, b;
-    __device__ __forceinline__ void load(const float *p) {
-        a = reinterpret_cast<const float4 *>(p)[0];
-        b = reinterpret_cast<const float4 *>(p)[1];
-    }
-    __device__ __forceinline__ void zero() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
-    __device__ __forceinline__ void get(float (&v)[8]) const {
-        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    template <bool HALVES>
+    __device__ __forceinline__ Pairs get() const {
+        auto lo = [](uint32_t x) { return __uint_as_float(x << 16); };
+        auto hi = [](uint32_t x) { return __uint_as_float(x & 0xffff0000u); };
+        if (HALVES) return Pairs{{pack2(lo(u.x), hi(u.x)), pack2(lo(u.y), hi(u.y))}, {pack2(lo(u.z), hi(u.z)), pack2(lo(u.w), hi(u.w))}};
+        return Pairs{{pack2(lo(u.x), lo(u.y)), pack2(lo(u.z), lo(u.w))}, {pack2(hi(u.x), hi(u.y)), pack2(hi(u.z), hi(u.w))}};
     }
 };
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
-    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);       // the result's one rounding
-    return *reinterpret_cast<const uint32_t *>(&v);
+template <> struct Raw<float> {
+    float4 u, v;
+    template <bool HALVES>
+    __device__ __forceinline__ void load(const float *row, const Channels &c) {
+        u = *reinterpret_cast<const float4 *>(row + c.lo);
+        v = *reinterpret_cast<const float4 *>(row + c.hi);
+    }
+    template <bool HALVES>
+    __device__ __forceinline__ Pairs get() const {
+        if (HALVES) return Pairs{{pack2(u.x, u.y), pack2(u.z, u.w)}, {pack2(v.x, v.y), pack2(v.z, v.w)}};
+        return Pairs{{pack2(u.x, u.z), pack2(v.x, v.z)}, {pack2(u.y, u.w), pack2(v.y, v.w)}};
+    }
+};
+// to a row's channels lo.. and hi..: the result's one rounding
+template <bool HALVES>
+__device__ __forceinline__ void put_pairs(__nv_bfloat16 *row, const Channels &c, const Pairs &v) {
+    float a[4], b[4];
+    unpack2(v.a[0], a[0], a[1]); unpack2(v.a[1], a[2], a[3]);
+    unpack2(v.b[0], b[0], b[1]); unpack2(v.b[1], b[2], b[3]);
+    if (HALVES) {
+        *reinterpret_cast<uint2 *>(row + c.lo) = make_uint2(tc::bf16x2(a[0], a[1]), tc::bf16x2(a[2], a[3]));
+        *reinterpret_cast<uint2 *>(row + c.hi) = make_uint2(tc::bf16x2(b[0], b[1]), tc::bf16x2(b[2], b[3]));
+    } else {
+        *reinterpret_cast<uint4 *>(row + c.lo) = make_uint4(tc::bf16x2(a[0], b[0]), tc::bf16x2(a[1], b[1]), tc::bf16x2(a[2], b[2]), tc::bf16x2(a[3], b[3]));
+    }
 }
-__device__ __forceinline__ void store8(__nv_bfloat16 *p, const float (&v)[8]) {
-    *reinterpret_cast<uint4 *>(p) = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
-}
-__device__ __forceinline__ void store8(float *p, const float (&v)[8]) {
-    reinterpret_cast<float4 *>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
-    reinterpret_cast<float4 *>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+template <bool HALVES>
+__device__ __forceinline__ void put_pairs(float *row, const Channels &c, const Pairs &v) {
+    float a[4], b[4];
+    unpack2(v.a[0], a[0], a[1]); unpack2(v.a[1], a[2], a[3]);
+    unpack2(v.b[0], b[0], b[1]); unpack2(v.b[1], b[2], b[3]);
+    *reinterpret_cast<float4 *>(row + c.lo) = HALVES ? make_float4(a[0], a[1], a[2], a[3]) : make_float4(a[0], b[0], a[1], b[1]);
+    *reinterpret_cast<float4 *>(row + c.hi) = HALVES ? make_float4(b[0], b[1], b[2], b[3]) : make_float4(a[2], b[2], a[3], b[3]);
 }
 
-// The angles of a lane's eight channels at one token: neighbours share an angle (interleaved pairs), or each channel has its own, whose
-// partner is n_pairs channels away (halves; sn then carries the sign of the partner's term).
-template <bool HALVES>
+// the angles of a lane's four pairs at one token
 struct Angles {
-    static constexpr int N = HALVES ? 8 : 4;
-    float cs[N], sn[N];
+    uint64_t cs[2], sn[2], neg[2];
     __device__ __forceinline__ void make(const double *s_turns, const uint8_t *s_axis, const int32_t *pos, int chunk, int n_pairs) {
+        float c[4], s[4];
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int ch = HALVES ? chunk * 8 + i : chunk * 4 + i;                 // channel, or pair
-            const int pair = HALVES && ch >= n_pairs ? ch - n_pairs : ch;
-            cs[i] = 1.f;
-            sn[i] = 0.f;
+        for (int i = 0; i < 4; ++i) {
+            const int pair = chunk * 4 + i;
+            c[i] = 1.f;
+            s[i] = 0.f;
             if (pair < n_pairs) {
                 const double t = (double)pos[s_axis[pair]] * s_turns[pair];
-                float s, c;
-                sincospif(2.f * (float)(t - rint(t)), &s, &c);
-                cs[i] = c;
-                sn[i] = HALVES && ch < n_pairs ? -s : s;
+                sincospif(2.f * (float)(t - rint(t)), &s[i], &c[i]);
             }
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            cs[k] = pack2(c[2 * k], c[2 * k + 1]);
+            sn[k] = pack2(s[2 * k], s[2 * k + 1]);
+            neg[k] = pack2(-s[2 * k], -s[2 * k + 1]);
         }
     }
-    // v <- the rotation of v (BACK: by the negative angle); partner: the lane that holds the other halves
-    template <bool BACK>
-    __device__ __forceinline__ void turn(float (&v)[8], int partner) const {
-        if constexpr (HALVES) {
+    // the rotation of v (BACK: by the negative angle); `turned`: which of the lane's pairs are, one bit each (FULL: all of every lane).  A
+    // channel that is not turned passes as it is: times a sine of zero, its neighbour's infinity would not be zero.
+    template <bool BACK, bool FULL>
+    __device__ __forceinline__ Pairs turn(const Pairs &v, int turned) const {
+        Pairs y;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float other = __shfl_sync(0xffffffffu, v[i], partner);
-                // (a channel that is not turned has sn = 0; its partner, itself, may hold an infinity)
-                const float t = sn[i] == 0.f ? 0.f : other * sn[i];
-                v[i] = v[i] * cs[i] + (BACK ? -t : t);
-            }
-        } else {
+        for (int k = 0; k < 2; ++k) {
+            const uint64_t up = BACK ? neg[k] : sn[k], down = BACK ? sn[k] : neg[k];
+            y.a[k] = fma2(v.b[k], down, mul2(v.a[k], cs[k]));
+            y.b[k] = fma2(v.a[k], up, mul2(v.b[k], cs[k]));
+        }
+        if (!FULL) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float a = v[2 * i], b = v[2 * i + 1], s = BACK ? -sn[i] : sn[i];
-                const float sb = sn[i] == 0.f ? 0.f : b * s, sa = sn[i] == 0.f ? 0.f : a * s;
-                v[2 * i] = a * cs[i] - sb;
-                v[2 * i + 1] = b * cs[i] + sa;
+            for (int k = 0; k < 2; ++k) {
+                float x0, x1, y0, y1;
+                const bool t0 = (turned >> (2 * k)) & 1, t1 = (turned >> (2 * k + 1)) & 1;
+                unpack2(v.a[k], x0, x1); unpack2(y.a[k], y0, y1);
+                y.a[k] = pack2(t0 ? y0 : x0, t1 ? y1 : x1);
+                unpack2(v.b[k], x0, x1); unpack2(y.b[k], y0, y1);
+                y.b[k] = pack2(t0 ? y0 : x0, t1 ? y1 : x1);
             }
         }
+        return y;
     }
 };
+__device__ __forceinline__ float sum2(uint64_t v) {
+    float a, b;
+    unpack2(v, a, b);
+    return a + b;
+}
 
 template <int LPR>
 __device__ __forceinline__ float row_sum(float v) {
@@ -150,53 +207,70 @@ __device__ __forceinline__ float row_sum(float v) {
     return v;
 }
 
-template <int D, bool HALVES, typename X, bool BWD>
-__global__ void __launch_bounds__(kRopeWarps * 32, BWD ? 2 : kRopeBlocksPerSm) norm_rope_kernel(const __grid_constant__ RopeTable tab, const RopeParams p) {
-    constexpr int LPR = D / 8, RPW = 32 / LPR;                 // lanes a row, rows a warp
-    constexpr int U = 4;                                       // rows of a lane under way
+// Rows of a lane under way, and blocks per SM: what the registers hold.
+template <typename X, bool BWD>
+struct RopeBatch {
+    static constexpr int U = sizeof(X) == 4 && BWD ? 2 : 4;
+    static constexpr int BLOCKS = BWD ? 2 : 3;
+};
+
+// FULL: every channel is turned
+template <int D, bool HALVES, bool FULL, typename X, bool BWD>
+__global__ void __launch_bounds__(kRopeWarps * 32, RopeBatch<X, BWD>::BLOCKS) norm_rope_kernel(const __grid_constant__ RopeTable tab, const RopeParams p) {
+    using RB = RopeBatch<X, BWD>;
+    using Y = typename std::conditional<BWD, X, __nv_bfloat16>::type;
+    constexpr int LPR = D / 8, RPW = 32 / LPR, U = RB::U;      // lanes a row, rows a warp
     __shared__ double s_turns[kMaxPairs];
     __shared__ uint8_t s_axis[kMaxPairs];
+    __shared__ __align__(16) float s_w[2][D];                  // in the order of the lanes' pairs
     __shared__ float s_dw[BWD ? kRopeWarps : 1][2][D];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, chunk = lane % LPR, sub = lane / LPR;
+    if (BWD) next_may_start();
     if (threadIdx.x < kMaxPairs) {
         s_turns[threadIdx.x] = tab.turns[threadIdx.x];
         s_axis[threadIdx.x] = tab.axis[threadIdx.x];
     }
+    for (int i = threadIdx.x; i < 2 * D; i += kRopeWarps * 32) {
+        const float *w = p.side[i / D].w;
+        s_w[i / D][i % D] = w ? w[Channels(HALVES, i % D / 8, p.n_pairs).of(HALVES, i & 3, (i >> 2) & 1)] : 1.f;
+    }
     __syncthreads();
-    // the lane of the other half of this lane's channels (whole chunks: n_pairs is a multiple of eight)
-    const int half = p.n_pairs >> 3;
-    const int partner = HALVES ? sub * LPR + (chunk < half ? chunk + half : chunk < 2 * half ? chunk - half : chunk) : lane;
-    float acc[2][8] = {};
+    const Channels ch(HALVES, chunk, p.n_pairs);
+    const int turned = p.n_pairs - chunk * 4 >= 4 ? 15 : p.n_pairs > chunk * 4 ? (1 << (p.n_pairs - chunk * 4)) - 1 : 0;
+    Angles ang;
+    Pairs acc[BWD ? 2 : 1] = {};
     const int64_t n_items = (int64_t)p.n_tokens * p.n_split;
     for (int64_t item = (int64_t)blockIdx.x * kRopeWarps + warp; item < n_items; item += (int64_t)gridDim.x * kRopeWarps) {
-        const int tok = (int)(item / p.n_split), part = (int)(item - (int64_t)tok * p.n_split);
-        const int u_end = min(p.units[0] + p.units[1], (part + 1) * p.per_warp);
-        Angles<HALVES> ang;
+        // (a token is split only where there are few: 32 bits will do)
+        const unsigned tok = p.n_split == 1 ? (unsigned)item : (unsigned)item / (unsigned)p.n_split;
+        const int share = (int)((unsigned)item - tok * (unsigned)p.n_split);
+        const int u_first = share * p.per_warp, u_end = min(p.units[0] + p.units[1], u_first + p.per_warp);
         bool made = false;
 #pragma unroll
         for (int z = 0; z < 2; ++z) {                          // queries, keys
-            const RopeSide &sd = p.side[z];
-            const int u0 = z ? p.units[0] : 0, first = max(part * p.per_warp, u0), last = min(u_end, u0 + p.units[z]);
+            const int u0 = z ? p.units[0] : 0, first = max(u_first, u0) - u0, last = min(u_end - u0, p.units[z]);
             if (first >= last) continue;
+            const RopeSide &sd = p.side[z];
             const bool norm = sd.w != nullptr;
-            float w[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) w[i] = norm ? sd.w[chunk * 8 + i] : 1.f;
-            const X *x = static_cast<const X *>(sd.x) + (int64_t)tok * sd.x_tok + chunk * 8;
-            const __nv_bfloat16 *dy = BWD ? sd.dy + (int64_t)tok * sd.dy_tok + chunk * 8 : nullptr;
+            int h = first * (U * RPW) + sub;                   // this lane's first head of the batch
+            const X *x = static_cast<const X *>(sd.x) + (int64_t)tok * sd.x_tok + (int64_t)h * sd.x_head;
+            const __nv_bfloat16 *dy = BWD ? sd.dy + (int64_t)tok * sd.dy_tok + (int64_t)h * sd.dy_head : nullptr;
+            Y *out = static_cast<Y *>(sd.out) + (int64_t)tok * sd.out_tok + (int64_t)h * sd.out_head;
+            const ulonglong2 wa = *reinterpret_cast<const ulonglong2 *>(&s_w[z][chunk * 8]), wb = *reinterpret_cast<const ulonglong2 *>(&s_w[z][chunk * 8 + 4]);
 #pragma unroll 1
-            for (int u = first; u < last; ++u) {
-                const int h0 = (u - u0) * (U * RPW) + sub;
-                Raw8<X> rx[U];
-                Raw8<__nv_bfloat16> rg[BWD ? U : 1];
+            for (int u = first; u < last; ++u, h += U * RPW) {
+                Raw<X> rx[U];
+                Raw<__nv_bfloat16> rg[BWD ? U : 1];
+                const int left = sd.heads - h;
 #pragma unroll
                 for (int y = 0; y < U; ++y) {
-                    const int h = h0 + y * RPW;
-                    rx[y].zero();
-                    if (h < sd.heads && (!BWD || norm)) rx[y].load(x + (int64_t)h * sd.x_head);
+                    rx[y] = {};
+                    if (y * RPW < left && (!BWD || norm)) rx[y].template load<HALVES>(x, ch);
+                    x += RPW * sd.x_head;
                     if constexpr (BWD) {
-                        rg[y].zero();
-                        if (h < sd.heads) rg[y].load(dy + (int64_t)h * sd.dy_head);
+                        rg[y] = {};
+                        if (y * RPW < left) rg[y].template load<HALVES>(dy, ch);
+                        dy += RPW * sd.dy_head;
                     }
                 }
                 if (!made) {                                   // while the first rows are on their way
@@ -205,41 +279,42 @@ __global__ void __launch_bounds__(kRopeWarps * 32, BWD ? 2 : kRopeBlocksPerSm) n
                 }
 #pragma unroll
                 for (int y = 0; y < U; ++y) {
-                    const int h = h0 + y * RPW;
-                    float v[8], r = 1.f;
-                    rx[y].get(v);
+                    Pairs v = rx[y].template get<HALVES>();
+                    uint64_t r2 = 0;
                     if (norm) {
-                        float ss = 0.f;
+                        const uint64_t ss = fma2(v.b[1], v.b[1], fma2(v.b[0], v.b[0], fma2(v.a[1], v.a[1], mul2(v.a[0], v.a[0]))));
+                        r2 = both(rsqrtf(row_sum<LPR>(sum2(ss)) * p.inv_d + p.eps));
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) ss = fmaf(v[i], v[i], ss);
-                        r = rsqrtf(row_sum<LPR>(ss) * p.inv_d + p.eps);
+                        for (int k = 0; k < 2; ++k) { v.a[k] = mul2(v.a[k], r2); v.b[k] = mul2(v.b[k], r2); }
                     }
                     if constexpr (!BWD) {
                         if (norm) {
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) v[i] = v[i] * r * w[i];
+                            v.a[0] = mul2(v.a[0], wa.x); v.a[1] = mul2(v.a[1], wa.y);
+                            v.b[0] = mul2(v.b[0], wb.x); v.b[1] = mul2(v.b[1], wb.y);
                         }
-                        ang.template turn<false>(v, partner);
-                        if (h < sd.heads) store8(static_cast<__nv_bfloat16 *>(sd.out) + (int64_t)h * sd.out_head + (int64_t)tok * sd.out_tok + chunk * 8, v);
+                        const Pairs t = ang.template turn<false, FULL>(v, turned);
+                        if (y * RPW < left) put_pairs<HALVES>(out, ch, t);
                     } else {
-                        float g[8];
-                        rg[y].get(g);
-                        ang.template turn<true>(g, partner);
+                        Pairs g = ang.template turn<true, FULL>(rg[y].template get<HALVES>(), turned);
                         if (norm) {
-                            float m = 0.f;
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) {
-                                v[i] *= r;
-                                acc[z][i] = fmaf(g[i], v[i], acc[z][i]);
-                                g[i] *= w[i];
-                                m = fmaf(g[i], v[i], m);
+                            for (int k = 0; k < 2; ++k) {
+                                acc[z].a[k] = fma2(g.a[k], v.a[k], acc[z].a[k]);
+                                acc[z].b[k] = fma2(g.b[k], v.b[k], acc[z].b[k]);
                             }
-                            m = row_sum<LPR>(m) * p.inv_d;
+                            g.a[0] = mul2(g.a[0], wa.x); g.a[1] = mul2(g.a[1], wa.y);
+                            g.b[0] = mul2(g.b[0], wb.x); g.b[1] = mul2(g.b[1], wb.y);
+                            const uint64_t m2 = fma2(g.b[1], v.b[1], fma2(g.b[0], v.b[0], fma2(g.a[1], v.a[1], mul2(g.a[0], v.a[0]))));
+                            const uint64_t nm = both(row_sum<LPR>(sum2(m2)) * -p.inv_d);
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) g[i] = r * (g[i] - v[i] * m);
+                            for (int k = 0; k < 2; ++k) {
+                                g.a[k] = mul2(fma2(v.a[k], nm, g.a[k]), r2);
+                                g.b[k] = mul2(fma2(v.b[k], nm, g.b[k]), r2);
+                            }
                         }
-                        if (h < sd.heads) store8(static_cast<X *>(sd.out) + (int64_t)h * sd.out_head + (int64_t)tok * sd.out_tok + chunk * 8, g);
+                        if (y * RPW < left) put_pairs<HALVES>(out, ch, g);
                     }
+                    out += RPW * sd.out_head;
                 }
             }
         }
@@ -247,14 +322,18 @@ __global__ void __launch_bounds__(kRopeWarps * 32, BWD ? 2 : kRopeBlocksPerSm) n
     if constexpr (BWD) {
         // the block's sums: the rows of a warp, then its warps, always in the same order
 #pragma unroll
-        for (int z = 0; z < 2; ++z)
+        for (int z = 0; z < 2; ++z) {
+            float f[8];
+            unpack2(acc[z].a[0], f[0], f[1]); unpack2(acc[z].a[1], f[2], f[3]);
+            unpack2(acc[z].b[0], f[4], f[5]); unpack2(acc[z].b[1], f[6], f[7]);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                float v = acc[z][i];
+                float v = f[i];
 #pragma unroll
                 for (int o = LPR; o < 32; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-                if (sub == 0) s_dw[warp][z][chunk * 8 + i] = v;
+                if (sub == 0) s_dw[warp][z][ch.of(HALVES, i & 3, i >> 2)] = v;
             }
+        }
         __syncthreads();
         if (threadIdx.x < 2 * D) {
             const int z = threadIdx.x / D, c = threadIdx.x % D;
@@ -271,9 +350,16 @@ __global__ void __launch_bounds__(1024) norm_rope_dw_kernel(const float *part, i
     __shared__ float s[32][33];
     const int groups = d / 32, z = blockIdx.x / groups, c = (blockIdx.x % groups) * 32 + (threadIdx.x & 31), y = threadIdx.x >> 5;
     float *dw = z ? dw_k : dw_q;
+    previous_done();                                            // launched early: the blocks' sums are there from here on
     if (!dw) return;
     float v = 0.f;
-    for (int b = y; b < n_blocks; b += 32) v += part[((size_t)b * 2 + z) * d + c];
+    for (int b = y; b < n_blocks; b += 256) {
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = b + 32 * i < n_blocks ? part[((size_t)(b + 32 * i) * 2 + z) * d + c] : 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v += x[i];
+    }
     s[y][threadIdx.x & 31] = v;
     __syncthreads();
     if (y == 0) {
@@ -287,10 +373,10 @@ __global__ void __launch_bounds__(1024) norm_rope_dw_kernel(const float *part, i
 // the most blocks that a backward launch has: what the workspace holds sums of
 constexpr int kRopeMaxBlocks = 2048;
 
-template <int D, bool HALVES, typename X, bool BWD>
+template <int D, bool HALVES, bool FULL, typename X, bool BWD>
 static int launch_norm_rope_t(const moc_rope *r, RopeParams &a, float *dw_q, float *dw_k, int n_sm, cudaStream_t s) {
-    constexpr int rows = 4 * 32 / (D / 8);
-    const int per_sm = BWD ? 2 : kRopeBlocksPerSm;
+    using RB = RopeBatch<X, BWD>;
+    constexpr int rows = RB::U * 32 / (D / 8), per_sm = RB::BLOCKS;      // rows of a batch
     for (int z = 0; z < 2; ++z) a.units[z] = (a.side[z].heads + rows - 1) / rows;
     const int units = a.units[0] + a.units[1];
     // A warp takes all of a token's heads, unless that leaves warps without work: then as many batches of rows as give every warp
@@ -301,10 +387,10 @@ static int launch_norm_rope_t(const moc_rope *r, RopeParams &a, float *dw_q, flo
     a.n_split = (units + a.per_warp - 1) / a.per_warp;
     const int64_t items = (int64_t)a.n_tokens * a.n_split;
     const unsigned grid = (unsigned)std::min<int64_t>({(items + kRopeWarps - 1) / kRopeWarps, (int64_t)n_sm * per_sm, (int64_t)kRopeMaxBlocks});
-    norm_rope_kernel<D, HALVES, X, BWD><<<grid, kRopeWarps * 32, 0, s>>>(r->tab, a);
+    norm_rope_kernel<D, HALVES, FULL, X, BWD><<<grid, kRopeWarps * 32, 0, s>>>(r->tab, a);
     MOC_LAUNCH_CHECK();
     if (BWD && (dw_q || dw_k)) {
-        norm_rope_dw_kernel<<<2 * D / 32, 1024, 0, s>>>(a.part, (int)grid, D, dw_q, dw_k);
+        MOC_CUDA_TRY(launch_early(true, norm_rope_dw_kernel, 2 * D / 32, 1024, 0, s, (const float *)a.part, (int)grid, D, dw_q, dw_k));
         MOC_LAUNCH_CHECK();
     }
     return MOC_OK;
@@ -323,14 +409,19 @@ static int launch_norm_rope(const moc_rope *r, RopeParams &a, int x_type, float 
         return MOC_OK;
     }
     a.n_axes = r->n_axes; a.n_pairs = r->n_pairs; a.eps = r->eps; a.inv_d = 1.f / r->d;
-    const bool halves = (r->flags & MOC_ROPE_HALVES) && r->n_pairs > 0, f32 = x_type == MOC_FP32;
-    using B = __nv_bfloat16;
-    if (r->d == 128) {
-        if (halves) return f32 ? launch_norm_rope_t<128, true, float, BWD>(r, a, dw_q, dw_k, n_sm, s) : launch_norm_rope_t<128, true, B, BWD>(r, a, dw_q, dw_k, n_sm, s);
-        return f32 ? launch_norm_rope_t<128, false, float, BWD>(r, a, dw_q, dw_k, n_sm, s) : launch_norm_rope_t<128, false, B, BWD>(r, a, dw_q, dw_k, n_sm, s);
-    }
-    if (halves) return f32 ? launch_norm_rope_t<64, true, float, BWD>(r, a, dw_q, dw_k, n_sm, s) : launch_norm_rope_t<64, true, B, BWD>(r, a, dw_q, dw_k, n_sm, s);
-    return f32 ? launch_norm_rope_t<64, false, float, BWD>(r, a, dw_q, dw_k, n_sm, s) : launch_norm_rope_t<64, false, B, BWD>(r, a, dw_q, dw_k, n_sm, s);
+    const bool halves = (r->flags & MOC_ROPE_HALVES) && r->n_pairs > 0, full = 2 * r->n_pairs == r->d;
+    // (all of them run the same code, with their sizes known to the compiler)
+    auto go = [&](auto d, auto halves_, auto full_, auto x) {
+        return launch_norm_rope_t<decltype(d)::value, decltype(halves_)::value, decltype(full_)::value, decltype(x), BWD>(r, a, dw_q, dw_k, n_sm, s);
+    };
+    using Yes = std::true_type;
+    using No = std::false_type;
+    auto by_pairs = [&](auto d, auto x) {
+        if (halves) return full ? go(d, Yes{}, Yes{}, x) : go(d, Yes{}, No{}, x);
+        return full ? go(d, No{}, Yes{}, x) : go(d, No{}, No{}, x);
+    };
+    auto by_type = [&](auto d) { return x_type == MOC_FP32 ? by_pairs(d, 0.f) : by_pairs(d, __nv_bfloat16()); };
+    return r->d == 128 ? by_type(std::integral_constant<int, 128>{}) : by_type(std::integral_constant<int, 64>{});
 }
 
 }  // namespace moc
