@@ -1,5 +1,5 @@
 // Cross attention to encoder states of another length (moc_cross_attend, moc_cross_attend_bwd): the plan, the entry points and the small
-// kernels that put shares together.  The attention itself: moc_cross_fwd_tc.cu, moc_cross_dq_tc.cu, moc_cross_dkv_tc.cu.
+// kernels that put shares together.  The attention itself: moc_cross_fwd_tc.cu, moc_cross_few.cu (few queries), moc_cross_dq_tc.cu, moc_cross_dkv_tc.cu.
 #include <string.h>
 
 #include <algorithm>
@@ -56,18 +56,19 @@ static int share_tiles(const std::vector<CrossItem> &items, int H, int n_sm, int
 }
 
 // cuts the items into shares of at most c key tiles; the longest items first
-static void cut_items(std::vector<CrossItem> &items, std::vector<CrossMerge> &merges, int &slots, int c) {
+static void cut_items(std::vector<CrossItem> &items, std::vector<CrossMerge> &merges, int &prows, int c) {
     std::vector<CrossItem> out;
     for (const CrossItem &i : items) {
         const int nt = (i.n_keys + 127) / 128, n = std::max(1, (nt + c - 1) / c);
         if (n == 1) { out.push_back(i); continue; }
-        merges.push_back(CrossMerge{i.q0, i.rows, slots, n});
+        merges.push_back(CrossMerge{i.q0, i.rows, prows, n});
         for (int x = 0; x < n; ++x) {
             const int t0 = (int)((int64_t)nt * x / n), t1 = (int)((int64_t)nt * (x + 1) / n);
             CrossItem p = i;
             p.k0 = i.k0 + t0 * 128;
             p.n_keys = std::min(i.n_keys, t1 * 128) - t0 * 128;
-            p.slot = slots++;
+            p.slot = prows;
+            prows += i.rows;
             out.push_back(p);
         }
     }
@@ -81,14 +82,44 @@ static void derive_cross(moc_cross *c, const moc_cross_problem *pr) {
     c->Lq = pr->q_off[S]; c->Lk = pr->k_off[S];
     c->scale = pr->softmax_scale != 0.f ? pr->softmax_scale : 1.f / std::sqrt((float)c->d);
     auto keys = [&](int s) { return pr->k_len ? pr->k_len[s] : pr->k_off[s + 1] - pr->k_off[s]; };
+    auto is_few = [&](int s) {
+        const int n = pr->q_off[s + 1] - pr->q_off[s];
+        return n > 0 && (int64_t)n * c->g <= kFewRows && keys(s) > 0;
+    };
+    // Few queries: shares of the states so that there are eight blocks for every SM (two to four are resident), of 128 states at least.
+    int64_t few_keys = 0;
+    for (int s = 0; s < S; ++s)
+        if (is_few(s)) few_keys += (int64_t)keys(s) * c->Hkv;
+    const int64_t few_share = std::max<int64_t>(128, (few_keys / (8 * c->n_sm) + 31) / 32 * 32);
     for (int s = 0; s < S; ++s) {
-        for (int q = pr->q_off[s]; q < pr->q_off[s + 1]; q += kCrossRows)
+        if (!is_few(s)) continue;
+        const int q_len = pr->q_off[s + 1] - pr->q_off[s], rows = q_len * c->g, blocks = (rows + 3) / 4, nk = keys(s);
+        const int n = (int)((nk + few_share - 1) / few_share);
+        for (int x = 0; x < n; ++x) {
+            const int k0 = (int)((int64_t)nk * x / n), k1 = (int)((int64_t)nk * (x + 1) / n);
+            for (int b = 0; b < blocks; ++b) {
+                const int r0 = rows * b / blocks, r1 = rows * (b + 1) / blocks;
+                c->few.push_back(CrossFew{pr->q_off[s], q_len, pr->k_off[s] + k0, k1 - k0, n > 1 ? c->prows + x * q_len : -1, r0, r1 - r0, 0});
+                c->few_rows = std::max(c->few_rows, r1 - r0);
+            }
+        }
+        if (n > 1) {
+            c->merges.push_back(CrossMerge{pr->q_off[s], q_len, c->prows, n});
+            c->prows += n * q_len;
+        }
+    }
+    std::stable_sort(c->few.begin(), c->few.end(), [](const CrossFew &a, const CrossFew &b) { return a.n_keys > b.n_keys; });
+    for (int s = 0; s < S; ++s) {
+        for (int q = pr->q_off[s]; !is_few(s) && q < pr->q_off[s + 1]; q += kCrossRows)
             c->items.push_back(CrossItem{q, std::min(kCrossRows, pr->q_off[s + 1] - q), pr->k_off[s], keys(s), -1, {}});
         for (int q = pr->q_off[s]; q < pr->q_off[s + 1]; q += 128)
             c->dq_items.push_back(CrossItem{q, std::min(128, pr->q_off[s + 1] - q), pr->k_off[s], keys(s), -1, {}});
     }
-    cut_items(c->items, c->merges, c->slots, share_tiles(c->items, c->H, c->n_sm, 128));
-    cut_items(c->dq_items, c->dq_merges, c->dq_slots, share_tiles(c->dq_items, c->H, c->n_sm, 0));
+    cut_items(c->items, c->merges, c->prows, share_tiles(c->items, c->H, c->n_sm, 128));
+    cut_items(c->dq_items, c->dq_merges, c->dq_prows, share_tiles(c->dq_items, c->H, c->n_sm, 0));
+    for (const CrossMerge &m : c->merges) c->most_merge_rows = std::max(c->most_merge_rows, m.rows);
+    for (const CrossItem &i : c->items) c->n_work += i.n_keys > 0;
+    for (const CrossItem &i : c->dq_items) c->n_dq_work += i.n_keys > 0;
 
     // Key-stationary pass.  The query tiles of a (key head, segment) are cut into parts of about the same length, and every key tile of
     // the segment against one part is a piece; a key tile with several parts is a sum of slots.  Pieces of the same part follow one another, so
@@ -152,32 +183,32 @@ static void derive_cross(moc_cross *c, const moc_cross_problem *pr) {
     const size_t H = c->H, d = c->d;
     w.status = 0;
     w.part_o = 256;
-    w.part_lse = up256(w.part_o + 4 * H * c->slots * kCrossRows * d);
-    w.fwd_end = up256(w.part_lse + 4 * H * c->slots * kCrossRows);
+    w.part_lse = up256(w.part_o + 4 * H * c->prows * d);
+    w.fwd_end = up256(w.part_lse + 4 * H * c->prows);
     w.delta = w.fwd_end;
     w.part_dq = up256(w.delta + 4 * H * c->Lq);
-    w.part_kv = up256(w.part_dq + 4 * H * c->dq_slots * 128 * d);
+    w.part_kv = up256(w.part_dq + 4 * H * c->dq_prows * d);
     w.bwd_end = up256(w.part_kv + 4 * 2 * (size_t)c->kv_slots * 128 * d);
 }
 
 // ---- shares of the forward: O = sum_i w_i O_i / sum_i w_i, w_i = exp(lse_i - max lse); a warp a row
 template <int D>
-__global__ void __launch_bounds__(256) cross_merge_kernel(const CrossMerge *merges, const float *part_o, const float *part_lse, int slots,
+__global__ void __launch_bounds__(256) cross_merge_kernel(const CrossMerge *merges, const float *part_o, const float *part_lse, int prows,
                                                           CrossRows O, float *lse, int Lq) {
     const CrossMerge m = merges[blockIdx.x];
     const int h = blockIdx.y, row = blockIdx.z * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
     if (row >= m.rows) return;
-    const size_t at = ((size_t)h * slots + m.slot) * kCrossRows + row;
+    const size_t at = (size_t)h * prows + m.slot + row;
     float big = -INFINITY;
-    for (int i = lane; i < m.n; i += 32) big = fmaxf(big, part_lse[at + (size_t)i * kCrossRows]);
+    for (int i = lane; i < m.n; i += 32) big = fmaxf(big, part_lse[at + (size_t)i * m.rows]);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, o));
     constexpr int V = D / 32;
     float acc[V] = {}, sum = 0.f;
     for (int i = 0; i < m.n; ++i) {
-        const float w = __expf(part_lse[at + (size_t)i * kCrossRows] - big);
+        const float w = __expf(part_lse[at + (size_t)i * m.rows] - big);
         sum += w;
-        const float *src = part_o + (at + (size_t)i * kCrossRows) * D + lane * V;
+        const float *src = part_o + (at + (size_t)i * m.rows) * D + lane * V;
 #pragma unroll
         for (int x = 0; x < V; x += 2) {
             const float2 v = *reinterpret_cast<const float2 *>(src + x);
@@ -206,11 +237,11 @@ __device__ __forceinline__ void sum_row(const float *src, size_t stride, int n, 
     *reinterpret_cast<uint2 *>(dst) = make_uint2(tc::bf16x2(acc.x, acc.y), tc::bf16x2(acc.z, acc.w));
 }
 template <int D>
-__global__ void __launch_bounds__(256) cross_sum_dq_kernel(const CrossMerge *merges, const float *part, int slots, CrossRows dQ) {
+__global__ void __launch_bounds__(256) cross_sum_dq_kernel(const CrossMerge *merges, const float *part, int prows, CrossRows dQ) {
     const CrossMerge m = merges[blockIdx.x];
     const int h = blockIdx.y, at = (blockIdx.z * 256 + threadIdx.x) * 4, row = at / D, col = at % D;
     if (row < m.rows)
-        sum_row<D>(part + (((size_t)h * slots + m.slot) * 128 + row) * D + col, (size_t)128 * D, m.n, dQ.row(h, m.q0 + row) + col);
+        sum_row<D>(part + ((size_t)h * prows + m.slot + row) * D + col, (size_t)m.rows * D, m.n, dQ.row(h, m.q0 + row) + col);
 }
 template <int D>
 __global__ void __launch_bounds__(256) cross_sum_kv_kernel(const CrossSum *sums, const float *part, CrossRows dK, CrossRows dV) {
@@ -250,11 +281,12 @@ extern "C" int moc_cross_create(const moc_cross_problem *pr, moc_cross **out) {
         auto take = [&](size_t bytes) { const size_t at = o; o = up256(o + bytes); return at; };
         const size_t a = take(sizeof(CrossItem) * c->items.size()), b = take(sizeof(CrossItem) * c->dq_items.size()),
                      m = take(sizeof(CrossMerge) * c->merges.size()), dm = take(sizeof(CrossMerge) * c->dq_merges.size()),
-                     p = take(sizeof(CrossPiece) * c->pieces.size()), po = take(4 * c->piece_off.size()), su = take(sizeof(CrossSum) * c->sums.size());
+                     fe = take(sizeof(CrossFew) * c->few.size()), p = take(sizeof(CrossPiece) * c->pieces.size()), po = take(4 * c->piece_off.size()), su = take(sizeof(CrossSum) * c->sums.size());
         std::vector<char> host(o);
         auto up = [&](size_t at, const void *src, size_t bytes) { if (bytes) memcpy(host.data() + at, src, bytes); };
         up(a, c->items.data(), sizeof(CrossItem) * c->items.size());
         up(b, c->dq_items.data(), sizeof(CrossItem) * c->dq_items.size());
+        up(fe, c->few.data(), sizeof(CrossFew) * c->few.size());
         up(m, c->merges.data(), sizeof(CrossMerge) * c->merges.size());
         up(dm, c->dq_merges.data(), sizeof(CrossMerge) * c->dq_merges.size());
         up(p, c->pieces.data(), sizeof(CrossPiece) * c->pieces.size());
@@ -279,7 +311,7 @@ extern "C" int moc_cross_create(const moc_cross_problem *pr, moc_cross **out) {
             return MOC_ERR_CUDA;
         }
         char *d = static_cast<char *>(c->d_blob);
-        c->d_items = (CrossItem *)(d + a); c->d_dq_items = (CrossItem *)(d + b);
+        c->d_items = (CrossItem *)(d + a); c->d_dq_items = (CrossItem *)(d + b); c->d_few = (CrossFew *)(d + fe);
         c->d_merges = (CrossMerge *)(d + m); c->d_dq_merges = (CrossMerge *)(d + dm);
         c->d_pieces = (CrossPiece *)(d + p); c->d_piece_off = (int32_t *)(d + po); c->d_sums = (CrossSum *)(d + su);
     } catch (...) {
@@ -317,12 +349,15 @@ extern "C" int moc_cross_attend(const moc_cross *c, const moc_rows *Q, const moc
         MOC_CUDA_TRY(cudaMemsetAsync(ws_ptr<int>(ws, c->ws.status), 0, 8, s));
         return MOC_OK;
     }
-    if (int r = launch_cross_fwd(c, Q, K, V, O, lse, ws, s)) return r;
+    if (!c->few.empty())
+        if (int r = launch_cross_few(c, Q, K, V, O, lse, ws, s)) return r;
+    if (!c->items.empty())
+        if (int r = launch_cross_fwd(c, Q, K, V, O, lse, ws, s)) return r;
     if (!c->merges.empty()) {
-        const dim3 grid((unsigned)c->merges.size(), c->H, kCrossRows / 8);
+        const dim3 grid((unsigned)c->merges.size(), c->H, (c->most_merge_rows + 7) / 8);
         const float *po = ws_ptr<float>(ws, c->ws.part_o), *pl = ws_ptr<float>(ws, c->ws.part_lse);
-        if (c->d == 128) cross_merge_kernel<128><<<grid, 256, 0, s>>>(c->d_merges, po, pl, c->slots, CrossRows(O), lse, c->Lq);
-        else cross_merge_kernel<64><<<grid, 256, 0, s>>>(c->d_merges, po, pl, c->slots, CrossRows(O), lse, c->Lq);
+        if (c->d == 128) cross_merge_kernel<128><<<grid, 256, 0, s>>>(c->d_merges, po, pl, c->prows, CrossRows(O), lse, c->Lq);
+        else cross_merge_kernel<64><<<grid, 256, 0, s>>>(c->d_merges, po, pl, c->prows, CrossRows(O), lse, c->Lq);
         MOC_LAUNCH_CHECK();
     }
     return MOC_OK;
@@ -344,8 +379,8 @@ extern "C" int moc_cross_attend_bwd(const moc_cross *c, const moc_rows *Q, const
         if (!c->dq_merges.empty()) {
             const dim3 g2((unsigned)c->dq_merges.size(), c->H, c->d / 8);      // 1024 values a block
             const float *part = ws_ptr<float>(ws, c->ws.part_dq);
-            if (c->d == 128) cross_sum_dq_kernel<128><<<g2, 256, 0, s>>>(c->d_dq_merges, part, c->dq_slots, CrossRows(dQ));
-            else cross_sum_dq_kernel<64><<<g2, 256, 0, s>>>(c->d_dq_merges, part, c->dq_slots, CrossRows(dQ));
+            if (c->d == 128) cross_sum_dq_kernel<128><<<g2, 256, 0, s>>>(c->d_dq_merges, part, c->dq_prows, CrossRows(dQ));
+            else cross_sum_dq_kernel<64><<<g2, 256, 0, s>>>(c->d_dq_merges, part, c->dq_prows, CrossRows(dQ));
             MOC_LAUNCH_CHECK();
         }
         if (!c->pieces.empty())

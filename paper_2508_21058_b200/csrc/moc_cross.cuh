@@ -7,9 +7,12 @@
 namespace moc {
 
 // A work item of the forward (up to 256 query rows of one segment) or of dQ (up to 128), of every head: its queries, its keys (n_keys
-// may be 0 in the forward), and where its share of the keys goes if there are other shares: the partial slot, -1 for none.
+// may be 0), and where its share's results go if there are other shares: the first row of partial results, -1 for none.
 struct __align__(16) CrossItem { int32_t q0, rows, k0, n_keys, slot, pad[3]; };
-// Rows whose partial results are put together: n slots from `slot` on.
+// A share of the states of a segment with few queries, of every key head: rows [r0, r0 + nr) of the q_len queries of each of the key
+// head's query heads; row r is query r mod q_len of query head r / q_len.
+struct __align__(16) CrossFew { int32_t q0, q_len, k0, n_keys, slot, r0, nr, pad; };
+// Rows whose partial results are put together: n times `rows`, from row `slot` of a head's partial results on.
 struct __align__(16) CrossMerge { int32_t q0, rows, slot, n; };
 // A piece of the key-stationary pass: up to 128 keys of a key head against units [u0, u1) of query rows; unit u: query head
 // h * group + u / q_tiles, rows q0 + 128 (u mod q_tiles) of the segment's [q0, q1).
@@ -18,13 +21,14 @@ struct __align__(16) CrossPiece { int32_t h, k0, keys, q0, q1, u0, u1, slot; };
 struct __align__(16) CrossSum { int32_t h, k0, rows, slot, n, pad[3]; };
 
 constexpr int kCrossRows = 256;
+constexpr int kFewRows = 8;        // rows of a key head up to which a segment counts as one with few queries
 
 struct CrossLayout {
     size_t status;
-    size_t part_o, part_lse;       // forward: [H][slots][256][d] and [H][slots][256] fp32
+    size_t part_o, part_lse;       // forward: [H][prows][d] and [H][prows] fp32
     size_t fwd_end;
     size_t delta;                  // [H][Lq]
-    size_t part_dq;                // [H][slots][128][d] fp32
+    size_t part_dq;                // [H][dq_prows][d] fp32
     size_t part_kv;                // [slots][2][128][d] fp32
     size_t bwd_end;
 };
@@ -39,9 +43,14 @@ struct moc_cross {
     std::vector<moc::CrossPiece> pieces;
     std::vector<int32_t> piece_off;                    // of every CTA of the key-stationary pass
     std::vector<moc::CrossSum> sums;
-    int slots = 0, dq_slots = 0, kv_slots = 0;         // per head, per head, in all
+    std::vector<moc::CrossFew> few;                    // per key head, the longest first
+    int few_rows = 0;                                  // the most rows that one has
+    int most_merge_rows = 0;                           // of the forward's merges
+    int prows = 0, dq_prows = 0, kv_slots = 0;         // rows of partial results of a head, the same of dQ; slots in all
+    int n_work = 0, n_dq_work = 0;                     // items that have keys: the others, which come last, only need zeros
     void *d_blob = nullptr;
     moc::CrossItem *d_items, *d_dq_items;
+    moc::CrossFew *d_few;
     moc::CrossMerge *d_merges, *d_dq_merges;
     moc::CrossPiece *d_pieces;
     int32_t *d_piece_off;
@@ -67,8 +76,17 @@ struct CrossRows {
 __device__ __forceinline__ int cross_item(int n) {
     return n * (int)gridDim.x + ((n & 1) ? (int)gridDim.x - 1 - (int)blockIdx.x : (int)blockIdx.x);
 }
+// how many of the first `n_all` items a CTA has
+__device__ __forceinline__ int cross_items(int n_all) {
+    const int rounds = n_all / (int)gridDim.x, rest = n_all - rounds * (int)gridDim.x;
+    return rounds + (((rounds & 1) ? (int)gridDim.x - 1 - (int)blockIdx.x : (int)blockIdx.x) < rest ? 1 : 0);
+}
+// asks for an item's description ahead of its use
+__device__ __forceinline__ void prefetch_item(const CrossItem *item) { asm volatile("prefetch.global.L1 [%0];" ::"l"(item)); }
 #endif
 
+int launch_cross_few(const moc_cross *c, const moc_rows *Q, const moc_rows *K, const moc_rows *V, const moc_rows *O, float *lse, void *ws,
+                     cudaStream_t s);
 int launch_cross_fwd(const moc_cross *c, const moc_rows *Q, const moc_rows *K, const moc_rows *V, const moc_rows *O, float *lse, void *ws,
                      cudaStream_t s);
 // (also writes delta)

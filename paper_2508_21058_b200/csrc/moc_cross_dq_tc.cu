@@ -26,11 +26,11 @@ using namespace tc;
 
 struct CrossDqParams {
     const CrossItem *items;
-    int n_all, H, g, Lq, slots;
+    int n_work, n_all, H, g, Lq, prows;      // items of all heads: with keys, all
     CrossRows K, V, O, dO, dQ;
     const float *lse;
     float *delta;                 // [H][Lq], written here for dK and dV
-    float *part;                  // [H][slots][128][D] shares of dQ
+    float *part;                  // [H][prows][D] shares of dQ
     int *status;
     float scale, scale_log2;
     WaitBound wait;
@@ -101,19 +101,13 @@ __global__ void __launch_bounds__(kCrossDqThreads, 1) cross_dq_tc_kernel(const _
     auto form_delta = [&](int dw) __attribute__((always_inline)) {
         constexpr int CH = D / 8, RP = 32 / CH, B = 4;         // lanes a row, rows an instruction, instructions under way
         const int sub = lane / CH, c16 = lane % CH;
-        int n_x = 0;
         bool ok = true;
-        for (int n = 0; ok; ++n) {
-            const int id = cross_item(n);
-            if (n * (int)gridDim.x >= p.n_all) break;
-            if (id >= p.n_all) continue;
-            const int rank = id / p.H, h = id - rank * p.H;
+        const int n_items = cross_items(p.n_work);
+        for (int n = 0; ok && n < n_items; ++n) {
+            const int id = cross_item(n), rank = id / p.H, h = id - rank * p.H;
             const CrossItem it = p.items[rank];
-            if (it.n_keys == 0) continue;
-            const int next = cross_item(n + 1);
-            if (next < p.n_all) {
-                const int nr = next / p.H, nh = next - nr * p.H;
-                const int q = p.items[nr].q0 + dw * 32 + lane;
+            if (n + 1 < n_items) {
+                const int next = cross_item(n + 1), nr = next / p.H, nh = next - nr * p.H, q = p.items[nr].q0 + dw * 32 + lane;
                 if (dw * 32 + lane < p.items[nr].rows)
 #pragma unroll
                     for (int x = 0; x < D / 64; ++x) {
@@ -130,8 +124,8 @@ __global__ void __launch_bounds__(kCrossDqThreads, 1) cross_dq_tc_kernel(const _
                     const int r = dw * 32 + r0 + y * RP + sub;
                     a[y] = b[y] = make_uint4(0, 0, 0, 0);
                     if (r < it.rows) {
-                        a[y] = *reinterpret_cast<const uint4 *>(p.O.row(h, it.q0 + r) + c16 * 8);
-                        b[y] = *reinterpret_cast<const uint4 *>(p.dO.row(h, it.q0 + r) + c16 * 8);
+                        a[y] = __ldcg(reinterpret_cast<const uint4 *>(p.O.row(h, it.q0 + r) + c16 * 8));      // (not through L1, where the items' descriptions are)
+                        b[y] = __ldcg(reinterpret_cast<const uint4 *>(p.dO.row(h, it.q0 + r) + c16 * 8));
                     }
                 }
 #pragma unroll
@@ -151,14 +145,19 @@ __global__ void __launch_bounds__(kCrossDqThreads, 1) cross_dq_tc_kernel(const _
                 }
             }
             if (dw * 32 + lane < it.rows) p.delta[(size_t)h * p.Lq + it.q0 + dw * 32 + lane] = mine;
-            if (n_x > 0) {
-                ok = __all_sync(0xffffffffu, mbar_wait(bar(X_EMPTY), (n_x - 1) & 1, abort_flag, p.wait, CQ_XEMPTY));
+            if (n > 0) {
+                ok = __all_sync(0xffffffffu, mbar_wait(bar(X_EMPTY), (n - 1) & 1, abort_flag, p.wait, CQ_XEMPTY));
                 if (!ok) break;
             }
-            s_ld[n_x & 1][1][dw * 32 + lane] = -mine;
+            s_ld[n & 1][1][dw * 32 + lane] = -mine;
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(X_FULL));
-            ++n_x;
+        }
+        // items without keys: dQ = 0
+        for (int id = p.n_work + blockIdx.x; id < p.n_all; id += gridDim.x) {
+            const int rank = id / p.H, h = id - rank * p.H, q0 = p.items[rank].q0, rows = p.items[rank].rows;
+            for (int x = dw * 32 + lane; x < rows * CH; x += 32 * kDeltaWarps)
+                *reinterpret_cast<uint4 *>(p.dQ.row(h, q0 + x / CH) + x % CH * 8) = make_uint4(0, 0, 0, 0);
         }
     };
 
@@ -168,120 +167,130 @@ __global__ void __launch_bounds__(kCrossDqThreads, 1) cross_dq_tc_kernel(const _
         const int r = threadIdx.x & 127, half = warp >> 2;
         const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
         const uint64_t c2 = pack2(p.scale_log2, p.scale_log2);
-        int gt = 0, n_done = 0;                           // tiles and items processed
-        bool ok = true;
-        for (int n = 0; ok; ++n) {
-            const int id = cross_item(n);
-            if (n * (int)gridDim.x >= p.n_all) break;
-            if (id >= p.n_all) continue;
-            const int rank = id / p.H, h = id - rank * p.H;
-            const CrossItem it = p.items[rank];
-            if (it.n_keys == 0) {
-                for (int x = threadIdx.x; x < it.rows * (D / 8); x += 256)
-                    *reinterpret_cast<uint4 *>(p.dQ.row(h, it.q0 + x / (D / 8)) + x % (D / 8) * 8) = make_uint4(0, 0, 0, 0);
-                continue;
-            }
-            ok = mbar_wait(bar(X_FULL), n_done & 1, abort_flag, p.wait, CQ_XFULL);
-            ok = __all_sync(0xffffffffu, ok);
-            if (!ok) break;
-            const float nlse = s_ld[n_done & 1][0][r], ndlt = s_ld[n_done & 1][1][r];
-            const uint64_t nlse2 = pack2(nlse, nlse), ndlt2 = pack2(ndlt, ndlt);
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar(X_EMPTY));
-            float pv[64];
-            bool t1_early = false;
-            for (int k = 0; k < it.n_keys; k += 128, ++gt) {
-                const int valid = min(128, it.n_keys - k), st = gt & 1;
-                const uint32_t t2 = tmem + lane_off + (st ? 384u : 128u);
-                ok = t1_early || mbar_wait_spin(bar(T1_FULL), gt & 1, abort_flag, p.wait, CQ_T1FULL);
+        int gt = 0;                                       // tiles processed
+        bool ok = true, t1_early = false;
+        // An item's results are read and stored behind the first tile of the next one: by then its last product has long landed.
+        int o_h = 0, o_q0 = 0, o_rows = 0, o_slot = 0;
+        const int n_items = cross_items(p.n_work);
+        for (int n = 0; ok && n_items > 0; ++n) {
+            const bool have = n < n_items;
+            int n_keys = 0, h = 0, q0 = 0, rows = 0, slot = 0;
+            uint64_t nlse2 = 0, ndlt2 = 0;
+            if (have) {
+                const int id = cross_item(n), rank = id / p.H;
+                const CrossItem it = p.items[rank];
+                h = id - rank * p.H; n_keys = it.n_keys; q0 = it.q0; rows = it.rows; slot = it.slot;
+                if (n + 1 < n_items && lane == 0) prefetch_item(p.items + cross_item(n + 1) / p.H);
+                ok = mbar_wait(bar(X_FULL), n & 1, abort_flag, p.wait, CQ_XFULL);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
-                tc_fence_after();
-                uint32_t sv[2][32];
-                tmem_ld32(tmem + lane_off + half * 32, sv[0]);
-                tmem_ld32(tmem + lane_off + (2 + half) * 32, sv[1]);
-                tmem_wait_ld();
-                tc_fence_before();
-                mbar_arrive(bar(T1_READ));                   // T1 may be overwritten
-                // (a barrier is looked at ahead of its wait, which costs some hundred cycles even if it has completed)
-                const bool t2_early = mbar_test_wait(bar(T2_FULL + st), (gt >> 1) & 1);
+                const float nlse = s_ld[n & 1][0][r], ndlt = s_ld[n & 1][1][r];
+                nlse2 = pack2(nlse, nlse);
+                ndlt2 = pack2(ndlt, ndlt);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(X_EMPTY));
+            }
+            int k = 0;
+            do {
+                if (have) {
+                    float pv[64];
+                    const int valid = min(128, n_keys - k), st = gt & 1;
+                    const uint32_t t2 = tmem + lane_off + (st ? 384u : 128u);
+                    ok = t1_early || mbar_wait_spin(bar(T1_FULL), gt & 1, abort_flag, p.wait, CQ_T1FULL);
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+                    tc_fence_after();
+                    uint32_t sv[2][32];
+                    tmem_ld32(tmem + lane_off + half * 32, sv[0]);
+                    tmem_ld32(tmem + lane_off + (2 + half) * 32, sv[1]);
+                    tmem_wait_ld();
+                    tc_fence_before();
+                    mbar_arrive(bar(T1_READ));                   // T1 may be overwritten
+                    // (a barrier is looked at ahead of its wait, which costs some hundred cycles even if it has completed)
+                    const bool t2_early = mbar_test_wait(bar(T2_FULL + st), (gt >> 1) & 1);
 #pragma unroll
-                for (int rd = 0; rd < 2; ++rd) {
-                    if (rd == 1 && valid <= 64) break;       // (ACC takes no step over these)
+                    for (int rd = 0; rd < 2; ++rd) {
+                        if (rd == 1 && valid <= 64) break;       // (ACC takes no step over these)
 #pragma unroll
-                    for (int x = 0; x < 32; x += 2) {
-                        float p0, p1;
-                        unpack2(fma2(pack2(__uint_as_float(sv[rd][x]), __uint_as_float(sv[rd][x + 1])), c2, nlse2), p0, p1);
-                        pv[rd * 32 + x] = ex2(p0);
-                        pv[rd * 32 + x + 1] = ex2(p1);
+                        for (int x = 0; x < 32; x += 2) {
+                            float p0, p1;
+                            unpack2(fma2(pack2(__uint_as_float(sv[rd][x]), __uint_as_float(sv[rd][x + 1])), c2, nlse2), p0, p1);
+                            pv[rd * 32 + x] = ex2(p0);
+                            pv[rd * 32 + x + 1] = ex2(p1);
+                        }
+                    }
+                    if (valid < 128) {
+#pragma unroll
+                        for (int x = 0; x < 64; ++x)
+                            if (((x >> 5) * 2 + half) * 32 + (x & 31) >= valid) pv[x] = 0.f;
+                    }
+                    ok = t2_early || mbar_wait_spin(bar(T2_FULL + st), (gt >> 1) & 1, abort_flag, p.wait, CQ_T2FULL);
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+                    tc_fence_after();
+                    uint32_t dp[2][32];
+                    tmem_ld32(t2 + half * 32, dp[0]);
+                    tmem_ld32(t2 + (2 + half) * 32, dp[1]);
+                    t1_early = mbar_test_wait(bar(T1_FULL), (gt + 1) & 1);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int rd = 0; rd < 2; ++rd) {
+                        if (rd == 1 && valid <= 64) break;
+                        uint32_t uds[16];
+#pragma unroll
+                        for (int x = 0; x < 32; x += 2) {
+                            float a0, a1;
+                            unpack2(mul2(pack2(pv[rd * 32 + x], pv[rd * 32 + x + 1]), add2(pack2(__uint_as_float(dp[rd][x]), __uint_as_float(dp[rd][x + 1])), ndlt2)), a0, a1);
+                            uds[x >> 1] = bf16x2(a0, a1);
+                        }
+                        tmem_st16(t2 + (rd * 2 + half) * 32, uds);
+                    }
+                    tmem_wait_st();
+                    tc_fence_before();
+                    mbar_arrive(bar(DS_DONE + st));
+                    ++gt;
+                }
+                if (k == 0 && n > 0) {
+                    // ---- the results of the item before: of the two warps that share the TMEM lanes, each takes 64 columns of all rows
+                    // (d = 128) or 16 rows (d = 64)
+                    ok = mbar_wait(bar(ACC_FULL), (n - 1) & 1, abort_flag, p.wait, CQ_ACCFULL);
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+                    tc_fence_after();
+                    constexpr int NJ = D / 32;                       // groups of eight rows that this warp has
+                    const int l4 = lane >> 2, l2 = lane & 3, cb = D == 128 ? half : 0, j0 = D == 128 ? 0 : 2 * half;
+                    uint32_t v[NJ / 2][32];
+#pragma unroll
+                    for (int x = 0; x < NJ / 2; ++x) tmem_ld_16x256b(tmem + lane_off + 256 + ((uint32_t)(x + (j0 >> 1)) << 20) + cb * 64, v[x]);
+                    tmem_wait_ld();
+                    tc_fence_before();
+                    mbar_arrive(bar(ACC_FREE));                      // this item's dQ may be accumulated
+#pragma unroll
+                    for (int y = 0; y < NJ; ++y) {
+                        const int row = (warp & 3) * 32 + (j0 + y) * 8 + l4;
+                        float f[16];
+#pragma unroll
+                        for (int x = 0; x < 8; ++x) {
+                            f[2 * x] = __uint_as_float(v[y >> 1][4 * x + 2 * (y & 1)]) * p.scale;
+                            f[2 * x + 1] = __uint_as_float(v[y >> 1][4 * x + 2 * (y & 1) + 1]) * p.scale;
+                        }
+                        if (o_slot < 0) {
+                            uint32_t u[8];
+#pragma unroll
+                            for (int x = 0; x < 8; ++x) u[x] = bf16x2(f[2 * x], f[2 * x + 1]);
+                            quad_transpose(u, l2);
+                            if (row < o_rows) store_quad(p.dQ.row(o_h, o_q0 + row) + cb * 64, l2, u);
+                        } else if (row < o_rows) {
+                            float *dst = p.part + ((size_t)o_h * p.prows + o_slot + row) * D + cb * 64 + 2 * l2;
+#pragma unroll
+                            for (int x = 0; x < 8; ++x) *reinterpret_cast<float2 *>(dst + 8 * x) = make_float2(f[2 * x], f[2 * x + 1]);
+                        }
                     }
                 }
-                if (valid < 128) {
-#pragma unroll
-                    for (int x = 0; x < 64; ++x)
-                        if (((x >> 5) * 2 + half) * 32 + (x & 31) >= valid) pv[x] = 0.f;
-                }
-                ok = t2_early || mbar_wait_spin(bar(T2_FULL + st), (gt >> 1) & 1, abort_flag, p.wait, CQ_T2FULL);
-                ok = __all_sync(0xffffffffu, ok);
-                if (!ok) break;
-                tc_fence_after();
-                uint32_t dp[2][32];
-                tmem_ld32(t2 + half * 32, dp[0]);
-                tmem_ld32(t2 + (2 + half) * 32, dp[1]);
-                t1_early = mbar_test_wait(bar(T1_FULL), (gt + 1) & 1);
-                tmem_wait_ld();
-#pragma unroll
-                for (int rd = 0; rd < 2; ++rd) {
-                    if (rd == 1 && valid <= 64) break;
-                    uint32_t uds[16];
-#pragma unroll
-                    for (int x = 0; x < 32; x += 2) {
-                        float a0, a1;
-                        unpack2(mul2(pack2(pv[rd * 32 + x], pv[rd * 32 + x + 1]), add2(pack2(__uint_as_float(dp[rd][x]), __uint_as_float(dp[rd][x + 1])), ndlt2)), a0, a1);
-                        uds[x >> 1] = bf16x2(a0, a1);
-                    }
-                    tmem_st16(t2 + (rd * 2 + half) * 32, uds);
-                }
-                tmem_wait_st();
-                tc_fence_before();
-                mbar_arrive(bar(DS_DONE + st));
-            }
-            if (!ok) break;
-            // ---- results: of the two warps that share the TMEM lanes, each takes 64 columns of all rows (d = 128) or 16 rows (d = 64)
-            ok = mbar_wait(bar(ACC_FULL), n_done & 1, abort_flag, p.wait, CQ_ACCFULL);
-            ok = __all_sync(0xffffffffu, ok);
-            if (!ok) break;
-            ++n_done;
-            tc_fence_after();
-            constexpr int NJ = D / 32;                       // groups of eight rows that this warp has
-            const int l4 = lane >> 2, l2 = lane & 3, cb = D == 128 ? half : 0, j0 = D == 128 ? 0 : 2 * half;
-            uint32_t v[NJ / 2][32];
-#pragma unroll
-            for (int x = 0; x < NJ / 2; ++x) tmem_ld_16x256b(tmem + lane_off + 256 + ((uint32_t)(x + (j0 >> 1)) << 20) + cb * 64, v[x]);
-            tmem_wait_ld();
-            tc_fence_before();
-            mbar_arrive(bar(ACC_FREE));                      // the next item's dQ may be accumulated
-#pragma unroll
-            for (int y = 0; y < NJ; ++y) {
-                const int row = (warp & 3) * 32 + (j0 + y) * 8 + l4;
-                float f[16];
-#pragma unroll
-                for (int x = 0; x < 8; ++x) {
-                    f[2 * x] = __uint_as_float(v[y >> 1][4 * x + 2 * (y & 1)]) * p.scale;
-                    f[2 * x + 1] = __uint_as_float(v[y >> 1][4 * x + 2 * (y & 1) + 1]) * p.scale;
-                }
-                if (it.slot < 0) {
-                    uint32_t u[8];
-#pragma unroll
-                    for (int x = 0; x < 8; ++x) u[x] = bf16x2(f[2 * x], f[2 * x + 1]);
-                    quad_transpose(u, l2);
-                    if (row < it.rows) store_quad(p.dQ.row(h, it.q0 + row) + cb * 64, l2, u);
-                } else if (row < it.rows) {
-                    float *dst = p.part + (((size_t)h * p.slots + it.slot) * 128 + row) * D + cb * 64 + 2 * l2;
-#pragma unroll
-                    for (int x = 0; x < 8; ++x) *reinterpret_cast<float2 *>(dst + 8 * x) = make_float2(f[2 * x], f[2 * x + 1]);
-                }
-            }
+                k += 128;
+            } while (k < n_keys);
+            if (!have) break;
+            o_h = h; o_q0 = q0; o_rows = rows; o_slot = slot;
         }
     } else if (warp == 8) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
@@ -313,11 +322,9 @@ __global__ void __launch_bounds__(kCrossDqThreads, 1) cross_dq_tc_kernel(const _
             }
             if (lane == 0) mbar_arrive(full);
         };
-        for (int n = 0; ok; ++n) {
-            const int id = cross_item(n);
-            if (n * (int)gridDim.x >= p.n_all) break;
-            if (id >= p.n_all) continue;
-            const int rank = id / p.H, hk = (id - rank * p.H) / p.g;
+        const int n_items = cross_items(p.n_work);
+        for (int n = 0; ok && n < n_items; ++n) {
+            const int id = cross_item(n), rank = id / p.H, hk = (id - rank * p.H) / p.g;
             const CrossItem it = p.items[rank];
             for (int k = 0; k < it.n_keys; k += 128) {
                 const int valid = min(128, it.n_keys - k), s2 = n_v & 1;
@@ -346,23 +353,19 @@ __global__ void __launch_bounds__(kCrossDqThreads, 1) cross_dq_tc_kernel(const _
             form_delta(warp - 10);
         } else {
             if (lane == 0) { prefetch_tensormap(&tmQ); prefetch_tensormap(&tmdO); }
-            int n_x = 0;
             bool ok = true;
-            for (int n = 0; ok; ++n) {
-                const int id = cross_item(n);
-                if (n * (int)gridDim.x >= p.n_all) break;
-                if (id >= p.n_all) continue;
-                const int rank = id / p.H, h = id - rank * p.H;
+            int n = 0;
+            for (const int n_items = cross_items(p.n_work); ok && n < n_items; ++n) {
+                const int id = cross_item(n), rank = id / p.H, h = id - rank * p.H;
                 const CrossItem it = p.items[rank];
-                if (it.n_keys == 0) continue;
                 float l[4];
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
                     const int r = x * 32 + lane;
                     l[x] = r < it.rows ? p.lse[(size_t)h * p.Lq + it.q0 + r] : INFINITY;       // rows that are not there: P = 0
                 }
-                if (n_x > 0) {
-                    ok = __all_sync(0xffffffffu, mbar_wait(bar(X_EMPTY), (n_x - 1) & 1, abort_flag, p.wait, CQ_XEMPTY));
+                if (n > 0) {
+                    ok = __all_sync(0xffffffffu, mbar_wait(bar(X_EMPTY), (n - 1) & 1, abort_flag, p.wait, CQ_XEMPTY));
                     if (!ok) break;
                 }
                 if (lane == 0) {
@@ -374,14 +377,13 @@ __global__ void __launch_bounds__(kCrossDqThreads, 1) cross_dq_tc_kernel(const _
                     }
                 }
 #pragma unroll
-                for (int x = 0; x < 4; ++x) s_ld[n_x & 1][0][x * 32 + lane] = l[x] * -1.4426950408889634f;
+                for (int x = 0; x < 4; ++x) s_ld[n & 1][0][x * 32 + lane] = l[x] * -1.4426950408889634f;
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(X_FULL));
-                ++n_x;
             }
-            if (*abort_flag && n_x > 0) {
+            if (*abort_flag && n > 0) {      // the last copies issued must land before the shared memory is released
                 int dummy_flag = 0;
-                mbar_wait(bar(X_FULL), (n_x - 1) & 1, &dummy_flag, p.wait, CQ_XFULL);
+                mbar_wait(bar(X_FULL), (n - 1) & 1, &dummy_flag, p.wait, CQ_XFULL);
             }
         }
     } else {
@@ -397,7 +399,7 @@ __global__ void __launch_bounds__(kCrossDqThreads, 1) cross_dq_tc_kernel(const _
             bool ok = true;
             auto wait = [&](int b, int parity, int code) { ok = ok && __all_sync(0xffffffffu, mbar_wait_spin(bar(b), parity, abort_flag, p.wait, code)); };
             auto n_of = [](int valid) { return (uint32_t)(valid + 15) & ~15u; };
-            int gt = 0, s3 = 0, ph3 = 0, n_x = 0;              // tile, its K stage and phase; items
+            int gt = 0, s3 = 0, ph3 = 0;                       // tile, its K stage and phase
             const bool side1 = uniform(warp) == 12;
             const uint64_t x1 = smem_desc_sw128(sX, 16, 1024), kk = smem_desc_sw128(sK, 16, 1024);
             const uint64_t x2 = smem_desc_sw128(sX + TILE_BYTES, 16, 1024), vv = smem_desc_sw128(sV, 16, 1024);
@@ -418,14 +420,10 @@ __global__ void __launch_bounds__(kCrossDqThreads, 1) cross_dq_tc_kernel(const _
                 tc_commit_elect(bar(V_EMPTY + s2));
                 if (last) tc_commit_elect(bar(X_EMPTY));
             };
-            for (int n = 0; ok; ++n) {
-                const int id = cross_item(n);
-                if (n * (int)gridDim.x >= p.n_all) break;
-                if (id >= p.n_all) continue;
-                const int n_keys = uniform(p.items[id / p.H].n_keys), n_tiles = (n_keys + 127) >> 7;
-                if (n_tiles == 0) continue;
+            for (int n = 0; ok && n < cross_items(p.n_work); ++n) {
+                const int n_keys = uniform(p.items[cross_item(n) / p.H].n_keys), n_tiles = (n_keys + 127) >> 7;
                 auto valid_of = [&](int j) { return min(128, n_keys - j * 128); };
-                wait(X_FULL, n_x & 1, CQ_XFULL);
+                wait(X_FULL, n & 1, CQ_XFULL);
                 if (!ok) break;
                 if (side1) {
                     for (int j = 0; ok && j < n_tiles; ++j, ++gt) {
@@ -449,7 +447,7 @@ __global__ void __launch_bounds__(kCrossDqThreads, 1) cross_dq_tc_kernel(const _
                     for (int j = 0; ok && j < n_tiles; ++j, ++gt) {
                         const int steps = (valid_of(j) + 15) >> 4;
                         wait(DS_DONE + (gt & 1), (gt >> 1) & 1, CQ_DSDONE);
-                        if (j == 0 && n_x > 0) wait(ACC_FREE, (n_x - 1) & 1, CQ_ACCFREE);      // the previous item's dQ has been read
+                        if (j == 0 && n > 0) wait(ACC_FREE, (n - 1) & 1, CQ_ACCFREE);      // the previous item's dQ has been read
                         if (!ok) break;
                         tc_fence_after();
                         const uint32_t ds = tmem + ((gt & 1) ? 384u : 128u);
@@ -463,7 +461,6 @@ __global__ void __launch_bounds__(kCrossDqThreads, 1) cross_dq_tc_kernel(const _
                     }
                     if (ok) tc_commit_elect(bar(ACC_FULL));
                 }
-                ++n_x;
             }
         }
     }
@@ -486,8 +483,8 @@ static int cross_dq_d(const moc_cross *c, const moc_rows *Q, const moc_rows *K, 
         if (int r = make_tmap_rows_bf16(&tmV16, V, c->Hkv, c->Lk, D, 16)) return r;
     }
     CrossDqParams a;
-    a.items = c->d_dq_items; a.n_all = (int)c->dq_items.size() * c->H;
-    a.H = c->H; a.g = c->g; a.Lq = c->Lq; a.slots = c->dq_slots;
+    a.items = c->d_dq_items; a.n_work = c->n_dq_work * c->H; a.n_all = (int)c->dq_items.size() * c->H;
+    a.H = c->H; a.g = c->g; a.Lq = c->Lq; a.prows = c->dq_prows;
     a.K = CrossRows(K); a.V = CrossRows(V); a.O = CrossRows(O); a.dO = CrossRows(dO); a.dQ = CrossRows(dQ);
     a.lse = lse; a.delta = ws_ptr<float>(ws, c->ws.delta);
     a.part = ws_ptr<float>(ws, c->ws.part_dq);

@@ -27,7 +27,7 @@ using namespace tc;
 struct CrossFwdParams {
     const CrossItem *items;
     int n_items, n_all;                // of a head, of all
-    int H, g, Lq, slots;
+    int H, g, Lq, prows;
     CrossRows V, O;
     float *lse, *part_o, *part_lse;
     int *status;
@@ -221,7 +221,7 @@ __global__ void __launch_bounds__(kCrossThreads, 1) cross_fwd_tc_kernel(const __
             const float inv_l = 1.f / l_run, lse = (m_run + log2f(l_run)) * 0.6931471805599453f;
             if (row < tile_rows) {
                 if (it.slot < 0) p.lse[(size_t)h * p.Lq + it.q0 + g * 128 + row] = lse;
-                else p.part_lse[((size_t)h * p.slots + it.slot) * kCrossRows + g * 128 + row] = lse;
+                else p.part_lse[(size_t)h * p.prows + it.slot + g * 128 + row] = lse;
             }
             ok = mbar_wait(bar(O_FULL + g), (bits & MINE_ODD) ? 1 : 0, abort_flag, p.wait, CW_OFULL);
             ok = __all_sync(0xffffffffu, ok);
@@ -254,7 +254,7 @@ __global__ void __launch_bounds__(kCrossThreads, 1) cross_fwd_tc_kernel(const __
                         quad_transpose(u, l2);
                         if (r < tile_rows) store_quad(p.O.row(h, it.q0 + g * 128 + r) + cb * 64, l2, u);
                     } else if (r < tile_rows) {
-                        float *dst = p.part_o + (((size_t)h * p.slots + it.slot) * kCrossRows + g * 128 + r) * D + cb * 64 + 2 * l2;
+                        float *dst = p.part_o + ((size_t)h * p.prows + it.slot + g * 128 + r) * D + cb * 64 + 2 * l2;
 #pragma unroll
                         for (int x = 0; x < 8; ++x) *reinterpret_cast<float2 *>(dst + 8 * x) = make_float2(f[2 * x], f[2 * x + 1]);
                     }
@@ -478,7 +478,7 @@ static int cross_fwd_d(const moc_cross *c, const moc_rows *Q, const moc_rows *K,
     }
     CrossFwdParams a;
     a.items = c->d_items; a.n_items = (int)c->items.size(); a.n_all = a.n_items * c->H;
-    a.H = c->H; a.g = c->g; a.Lq = c->Lq; a.slots = c->slots;
+    a.H = c->H; a.g = c->g; a.Lq = c->Lq; a.prows = c->prows;
     a.V = CrossRows(V); a.O = CrossRows(O); a.lse = lse;
     a.part_o = ws_ptr<float>(ws, c->ws.part_o); a.part_lse = ws_ptr<float>(ws, c->ws.part_lse);
     a.status = ws_ptr<int>(ws, c->ws.status);

@@ -25,6 +25,13 @@ CASES = [
     (6, 2, 128, [513, 0, 31], [40, 50, 0], 0),
     (8, 8, 64, [2000, 3], [512, 512], 0),
     (16, 4, 128, [1300, 640], [333, 512], 7),           # more items than SMs
+    # few queries: up to eight rows of the query heads that share a key head, one to four in a block
+    (8, 1, 64, [1, 1], [3000, 5], 0),
+    (8, 1, 128, [1, 1, 300], [3000, 5, 70], 3),
+    (2, 2, 128, [2, 4, 8, 9], [700, 129, 40, 200], 1),
+    (4, 2, 64, [3, 0, 1], [1000, 9, 31], 2),
+    (5, 5, 128, [1], [4097], 0),
+    (7, 1, 128, [1, 1], [33, 640], 0),
 ]
 
 
