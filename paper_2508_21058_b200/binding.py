@@ -274,36 +274,38 @@ class MocPlan:
         return desc, sel, O, lse, ws
 
 
-def _rows(t, heads, tokens, d, dtype, name):
-    """A [heads][tokens][d] tensor of any strides as the library takes it."""
-    if t.dtype is not dtype or t.shape != (heads, tokens, d):
-        raise MocError(-2, f"moc error -2: {name} is {t.dtype} {tuple(t.shape)}, not {dtype} {(heads, tokens, d)}")
-    head, tok, one = t.stride()
-    if one != 1:
+def _rows(t, heads, tokens, d, dtype, name, dev, spare=False):
+    """A [heads][tokens][d] tensor of any strides as the library takes it; `spare`: it may have more tokens."""
+    shape = t.shape
+    if t.dtype is dtype and t.get_device() == dev and len(shape) == 3 and shape[0] == heads and shape[2] == d and (
+            shape[1] == tokens or (spare and shape[1] > tokens)):
+        head, tok, one = t.stride()
+        if one == 1:
+            return _Rows(t.data_ptr(), head, tok)
         raise MocError(-2, f"moc error -2: the channels of {name} are not consecutive")
-    _on_current(t, name)
-    return _Rows(t.data_ptr(), head, tok)
+    _on_current(t, name, dev)
+    raise MocError(-2, f"moc error -2: {name} is {t.dtype} {tuple(shape)}, not {dtype} {(heads, tokens, d)}")
 
 
-def _on_current(t, name):
-    if t.get_device() != torch._C._cuda_getDevice():           # (-1 on the CPU)
+def _on_current(t, name, dev):
+    if t.get_device() != dev:                                   # (-1 on the CPU)
         raise MocError(-6, f"moc error -6: {name} is on {t.device}, which is not the current device")
 
 
-def _table(t, shape, dtype, name):
+def _table(t, shape, dtype, name, dev):
     """The address of a contiguous tensor, or NULL."""
     if t is None:
         return None
     if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
         raise MocError(-2, f"moc error -2: {name} is {t.dtype} {tuple(t.shape)}, not contiguous {dtype} {shape}")
-    _on_current(t, name)
+    _on_current(t, name, dev)
     return t.data_ptr()
 
 
-def _scratch(ws, n_bytes):
+def _scratch(ws, n_bytes, dev):
     if ws is None or ws.numel() * ws.element_size() < n_bytes or not ws.is_contiguous():
         raise MocError(-5, f"moc error -5: a contiguous workspace of {n_bytes} bytes is needed")
-    _on_current(ws, "the workspace")
+    _on_current(ws, "the workspace", dev)
     return ws.data_ptr()
 
 
@@ -357,32 +359,41 @@ class MocRope:
     def new_workspace(self, device="cuda") -> torch.Tensor:
         return torch.empty(self._ws_bytes, dtype=torch.uint8, device=device)
 
-    def _common(self, pos, q, k):
-        L = q.shape[1]
-        if q.dtype not in (torch.bfloat16, torch.float32):
-            raise MocError(-2, f"moc error -2: queries are bf16 or fp32, not {q.dtype}")
-        return (1 if q.dtype == torch.float32 else 0, L, q.shape[0], 0 if k is None else k.shape[0],
-                _table(pos, (L, self.n_axes), torch.int32, "pos") if self.n_axes else None)
+    def _common(self, pos, q, k, dev):
+        if q.dim() != 3 or q.dtype not in (torch.bfloat16, torch.float32):
+            raise MocError(-2, f"moc error -2: queries are [head][token][d], bf16 or fp32, not {q.dtype} {tuple(q.shape)}")
+        if k is not None and k.dim() != 3:
+            raise MocError(-2, f"moc error -2: keys are [head][token][d], not {tuple(k.shape)}")
+        hq, L, _ = q.shape
+        return (1 if q.dtype is torch.float32 else 0, L, hq, 0 if k is None else k.shape[0],
+                _table(pos, (L, self.n_axes), torch.int32, "pos", dev) if self.n_axes else None)
 
     def moc_norm_rope(self, pos, q, w_q, q_out, k=None, w_k=None, k_out=None):
         """q_out (and k_out) <- norm and rotation of q (and k); pos: int32 [token][axis]; w_q, w_k: fp32 [d], or None for no norm."""
-        x_type, L, hq, hk, at = self._common(pos, q, k)
-        b16, d = torch.bfloat16, self.d
-        rk = (_rows(k, hk, L, d, q.dtype, "k"), _table(w_k, (d,), torch.float32, "w_k"), _rows(k_out, hk, L, d, b16, "k_out")) if hk else (None,) * 3
-        _check(self._lib.moc_norm_rope(self._h, x_type, L, hq, hk, at, _rows(q, hq, L, d, q.dtype, "q"), _table(w_q, (d,), torch.float32, "w_q"),
-                                       _rows(q_out, hq, L, d, b16, "q_out"), *rk, _stream()))
+        dev, d, b16, f32 = torch._C._cuda_getDevice(), self.d, torch.bfloat16, torch.float32
+        x_type, L, hq, hk, at = self._common(pos, q, k, dev)
+        rk = (None,) * 3
+        if hk:
+            rk = (_rows(k, hk, L, d, q.dtype, "k", dev), _table(w_k, (d,), f32, "w_k", dev), _rows(k_out, hk, L, d, b16, "k_out", dev))
+        code = self._lib.moc_norm_rope(self._h, x_type, L, hq, hk, at, _rows(q, hq, L, d, q.dtype, "q", dev), _table(w_q, (d,), f32, "w_q", dev),
+                                       _rows(q_out, hq, L, d, b16, "q_out", dev), *rk, torch._C._cuda_getCurrentRawStream(dev))
+        if code:
+            _check(code)
 
     def moc_norm_rope_bwd(self, pos, q, w_q, dq_out, dq, dw_q, ws, k=None, w_k=None, dk_out=None, dk=None, dw_k=None):
         """dq, dw_q (and dk, dw_k) <- from dq_out (and dk_out), the gradients of moc_norm_rope's outputs."""
-        x_type, L, hq, hk, at = self._common(pos, q, k)
-        b16, d, f32 = torch.bfloat16, self.d, torch.float32
+        dev, d, b16, f32 = torch._C._cuda_getDevice(), self.d, torch.bfloat16, torch.float32
+        x_type, L, hq, hk, at = self._common(pos, q, k, dev)
         rk = (None,) * 5
         if hk:
-            rk = (_rows(k, hk, L, d, q.dtype, "k"), _table(w_k, (d,), f32, "w_k"), _rows(dk_out, hk, L, d, b16, "dk_out"),
-                  _rows(dk, hk, L, d, q.dtype, "dk"), _table(dw_k, (d,), f32, "dw_k"))
-        _check(self._lib.moc_norm_rope_bwd(self._h, x_type, L, hq, hk, at, _rows(q, hq, L, d, q.dtype, "q"), _table(w_q, (d,), f32, "w_q"),
-                                           _rows(dq_out, hq, L, d, b16, "dq_out"), _rows(dq, hq, L, d, q.dtype, "dq"), _table(dw_q, (d,), f32, "dw_q"),
-                                           *rk, _scratch(ws, self._ws_bytes), _stream()))
+            rk = (_rows(k, hk, L, d, q.dtype, "k", dev), _table(w_k, (d,), f32, "w_k", dev), _rows(dk_out, hk, L, d, b16, "dk_out", dev),
+                  _rows(dk, hk, L, d, q.dtype, "dk", dev), _table(dw_k, (d,), f32, "dw_k", dev))
+        code = self._lib.moc_norm_rope_bwd(self._h, x_type, L, hq, hk, at, _rows(q, hq, L, d, q.dtype, "q", dev), _table(w_q, (d,), f32, "w_q", dev),
+                                           _rows(dq_out, hq, L, d, b16, "dq_out", dev), _rows(dq, hq, L, d, q.dtype, "dq", dev),
+                                           _table(dw_q, (d,), f32, "dw_q", dev), *rk, _scratch(ws, self._ws_bytes, dev),
+                                           torch._C._cuda_getCurrentRawStream(dev))
+        if code:
+            _check(code)
 
 
 class MocCross:
@@ -425,26 +436,28 @@ class MocCross:
     def new_workspace(self, with_bwd=False, device="cuda") -> torch.Tensor:
         return torch.empty(self.workspace_bytes(with_bwd), dtype=torch.uint8, device=device)
 
-    def _q(self, t, name):       # (a tensor may have more rows than the segments: those behind the last one's are left alone)
-        if t.dim() == 3 and t.shape[1] < self.n_queries:
-            raise MocError(-2, f"moc error -2: {name} has {t.shape[1]} rows, the segments {self.n_queries}")
-        return _rows(t, self.H, t.shape[1] if t.dim() == 3 else self.n_queries, self.d, torch.bfloat16, name)
-
-    def _k(self, t, name):
-        if t.dim() == 3 and t.shape[1] < self.n_states:
-            raise MocError(-2, f"moc error -2: {name} has {t.shape[1]} rows, the segments {self.n_states}")
-        return _rows(t, self.Hkv, t.shape[1] if t.dim() == 3 else self.n_states, self.d, torch.bfloat16, name)
-
+    # (tensors may have more rows than the segments: those behind the last one's are left alone)
     def moc_cross_attend(self, Q, K, V, O, lse, ws):
         """O, lse (fp32 [head][query]) <- attention of every segment's queries to its states."""
-        _check(self._lib.moc_cross_attend(self._h, self._q(Q, "Q"), self._k(K, "K"), self._k(V, "V"), self._q(O, "O"),
-                                          _table(lse, (self.H, self.n_queries), torch.float32, "lse"), _scratch(ws, self._ws_bytes[0]), _stream()))
+        dev, H, kv, n, m, d, b16 = torch._C._cuda_getDevice(), self.H, self.Hkv, self.n_queries, self.n_states, self.d, torch.bfloat16
+        code = self._lib.moc_cross_attend(self._h, _rows(Q, H, n, d, b16, "Q", dev, True), _rows(K, kv, m, d, b16, "K", dev, True),
+                                          _rows(V, kv, m, d, b16, "V", dev, True), _rows(O, H, n, d, b16, "O", dev, True),
+                                          _table(lse, (H, n), torch.float32, "lse", dev), _scratch(ws, self._ws_bytes[0], dev),
+                                          torch._C._cuda_getCurrentRawStream(dev))
+        if code:
+            _check(code)
 
     def moc_cross_attend_bwd(self, Q, K, V, O, lse, dO, dQ, dK, dV, ws):
         """dQ, dK, dV <- from dO, the gradient of O; O, lse: the forward's."""
-        _check(self._lib.moc_cross_attend_bwd(self._h, self._q(Q, "Q"), self._k(K, "K"), self._k(V, "V"), self._q(O, "O"),
-                                              _table(lse, (self.H, self.n_queries), torch.float32, "lse"), self._q(dO, "dO"), self._q(dQ, "dQ"),
-                                              self._k(dK, "dK"), self._k(dV, "dV"), _scratch(ws, self._ws_bytes[1]), _stream()))
+        dev, H, kv, n, m, d, b16 = torch._C._cuda_getDevice(), self.H, self.Hkv, self.n_queries, self.n_states, self.d, torch.bfloat16
+        code = self._lib.moc_cross_attend_bwd(self._h, _rows(Q, H, n, d, b16, "Q", dev, True), _rows(K, kv, m, d, b16, "K", dev, True),
+                                              _rows(V, kv, m, d, b16, "V", dev, True), _rows(O, H, n, d, b16, "O", dev, True),
+                                              _table(lse, (H, n), torch.float32, "lse", dev), _rows(dO, H, n, d, b16, "dO", dev, True),
+                                              _rows(dQ, H, n, d, b16, "dQ", dev, True), _rows(dK, kv, m, d, b16, "dK", dev, True),
+                                              _rows(dV, kv, m, d, b16, "dV", dev, True), _scratch(ws, self._ws_bytes[1], dev),
+                                              torch._C._cuda_getCurrentRawStream(dev))
+        if code:
+            _check(code)
 
     def moc_cross_get_status(self, ws):
         st, det = C.c_int(0), C.c_int(0)

@@ -191,12 +191,25 @@ static void derive_cross(moc_cross *c, const moc_cross_problem *pr) {
     w.bwd_end = up256(w.part_kv + 4 * 2 * (size_t)c->kv_slots * 128 * d);
 }
 
-// ---- shares of the forward: O = sum_i w_i O_i / sum_i w_i, w_i = exp(lse_i - max lse); a warp a row
+// The launches that put shares together begin while the one before them still runs, and wait for its results.
+template <typename... P, typename... A>
+static cudaError_t launch_after(void (*kernel)(P...), dim3 grid, cudaStream_t s, A &&...args) {
+    cudaLaunchAttribute at;
+    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t c = {};
+    c.gridDim = grid; c.blockDim = dim3(256); c.stream = s;
+    c.attrs = &at; c.numAttrs = 1;
+    return cudaLaunchKernelEx(&c, kernel, std::forward<A>(args)...);
+}
+
+// ---- shares of the forward: O = sum_i w_i O_i / sum_i w_i, w_i = exp(lse_i - max lse); a warp a row, four shares' loads under way
 template <int D>
 __global__ void __launch_bounds__(256) cross_merge_kernel(const CrossMerge *merges, const float *part_o, const float *part_lse, int prows,
                                                           CrossRows O, float *lse, int Lq) {
     const CrossMerge m = merges[blockIdx.x];
     const int h = blockIdx.y, row = blockIdx.z * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    previous_done();
     if (row >= m.rows) return;
     const size_t at = (size_t)h * prows + m.slot + row;
     float big = -INFINITY;
@@ -205,15 +218,26 @@ __global__ void __launch_bounds__(256) cross_merge_kernel(const CrossMerge *merg
     for (int o = 16; o > 0; o >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, o));
     constexpr int V = D / 32;
     float acc[V] = {}, sum = 0.f;
-    for (int i = 0; i < m.n; ++i) {
-        const float w = __expf(part_lse[at + (size_t)i * m.rows] - big);
-        sum += w;
-        const float *src = part_o + (at + (size_t)i * m.rows) * D + lane * V;
+    for (int i = 0; i < m.n; i += 4) {
+        float2 v[4][V / 2];
+        float w[4];
 #pragma unroll
-        for (int x = 0; x < V; x += 2) {
-            const float2 v = *reinterpret_cast<const float2 *>(src + x);
-            acc[x] = fmaf(w, v.x, acc[x]);
-            acc[x + 1] = fmaf(w, v.y, acc[x + 1]);
+        for (int x = 0; x < 4; ++x) {
+            const size_t src = at + (size_t)min(i + x, m.n - 1) * m.rows;
+            w[x] = part_lse[src];
+#pragma unroll
+            for (int y = 0; y < V / 2; ++y) v[x][y] = *reinterpret_cast<const float2 *>(part_o + src * D + lane * V + 2 * y);
+        }
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            if (i + x >= m.n) break;
+            const float e = __expf(w[x] - big);
+            sum += e;
+#pragma unroll
+            for (int y = 0; y < V / 2; ++y) {
+                acc[2 * y] = fmaf(e, v[x][y].x, acc[2 * y]);
+                acc[2 * y + 1] = fmaf(e, v[x][y].y, acc[2 * y + 1]);
+            }
         }
     }
     const float inv = 1.f / sum;
@@ -240,6 +264,7 @@ template <int D>
 __global__ void __launch_bounds__(256) cross_sum_dq_kernel(const CrossMerge *merges, const float *part, int prows, CrossRows dQ) {
     const CrossMerge m = merges[blockIdx.x];
     const int h = blockIdx.y, at = (blockIdx.z * 256 + threadIdx.x) * 4, row = at / D, col = at % D;
+    previous_done();
     if (row < m.rows)
         sum_row<D>(part + ((size_t)h * prows + m.slot + row) * D + col, (size_t)m.rows * D, m.n, dQ.row(h, m.q0 + row) + col);
 }
@@ -247,6 +272,7 @@ template <int D>
 __global__ void __launch_bounds__(256) cross_sum_kv_kernel(const CrossSum *sums, const float *part, CrossRows dK, CrossRows dV) {
     const CrossSum m = sums[blockIdx.x];
     const int side = blockIdx.y, at = (blockIdx.z * 256 + threadIdx.x) * 4, row = at / D, col = at % D;
+    previous_done();
     if (row < m.rows)
         sum_row<D>(part + (((size_t)m.slot * 2 + side) * 128 + row) * D + col, (size_t)2 * 128 * D, m.n, (side ? dV : dK).row(m.h, m.k0 + row) + col);
 }
@@ -356,8 +382,8 @@ extern "C" int moc_cross_attend(const moc_cross *c, const moc_rows *Q, const moc
     if (!c->merges.empty()) {
         const dim3 grid((unsigned)c->merges.size(), c->H, (c->most_merge_rows + 7) / 8);
         const float *po = ws_ptr<float>(ws, c->ws.part_o), *pl = ws_ptr<float>(ws, c->ws.part_lse);
-        if (c->d == 128) cross_merge_kernel<128><<<grid, 256, 0, s>>>(c->d_merges, po, pl, c->prows, CrossRows(O), lse, c->Lq);
-        else cross_merge_kernel<64><<<grid, 256, 0, s>>>(c->d_merges, po, pl, c->prows, CrossRows(O), lse, c->Lq);
+        MOC_CUDA_TRY(launch_after(c->d == 128 ? cross_merge_kernel<128> : cross_merge_kernel<64>, grid, s, (const CrossMerge *)c->d_merges, po, pl, c->prows,
+                                  CrossRows(O), lse, c->Lq));
         MOC_LAUNCH_CHECK();
     }
     return MOC_OK;
@@ -379,8 +405,8 @@ extern "C" int moc_cross_attend_bwd(const moc_cross *c, const moc_rows *Q, const
         if (!c->dq_merges.empty()) {
             const dim3 g2((unsigned)c->dq_merges.size(), c->H, c->d / 8);      // 1024 values a block
             const float *part = ws_ptr<float>(ws, c->ws.part_dq);
-            if (c->d == 128) cross_sum_dq_kernel<128><<<g2, 256, 0, s>>>(c->d_dq_merges, part, c->dq_prows, CrossRows(dQ));
-            else cross_sum_dq_kernel<64><<<g2, 256, 0, s>>>(c->d_dq_merges, part, c->dq_prows, CrossRows(dQ));
+            MOC_CUDA_TRY(launch_after(c->d == 128 ? cross_sum_dq_kernel<128> : cross_sum_dq_kernel<64>, g2, s, (const CrossMerge *)c->d_dq_merges, part,
+                                      c->dq_prows, CrossRows(dQ)));
             MOC_LAUNCH_CHECK();
         }
         if (!c->pieces.empty())
@@ -391,8 +417,8 @@ extern "C" int moc_cross_attend_bwd(const moc_cross *c, const moc_rows *Q, const
     if (!c->sums.empty()) {
         const dim3 g3((unsigned)c->sums.size(), 2, c->d / 8);
         const float *part = ws_ptr<float>(ws, c->ws.part_kv);
-        if (c->d == 128) cross_sum_kv_kernel<128><<<g3, 256, 0, s>>>(c->d_sums, part, CrossRows(dK), CrossRows(dV));
-        else cross_sum_kv_kernel<64><<<g3, 256, 0, s>>>(c->d_sums, part, CrossRows(dK), CrossRows(dV));
+        MOC_CUDA_TRY(launch_after(c->d == 128 ? cross_sum_kv_kernel<128> : cross_sum_kv_kernel<64>, g3, s, (const CrossSum *)c->d_sums, part, CrossRows(dK),
+                                  CrossRows(dV)));
         MOC_LAUNCH_CHECK();
     }
     return MOC_OK;

@@ -66,6 +66,7 @@ __global__ void __launch_bounds__(kCrossKvThreads, 1) cross_dkv_tc_kernel(const 
         if (threadIdx.x == 0) report_abort(p.status, CB_SMEM);
         return;
     }
+    next_may_start();
     if (threadIdx.x == 0) {
         s_abort = 0;
         for (int b = 0; b < N_BARS; ++b)

@@ -69,6 +69,7 @@ __global__ void __launch_bounds__(kCrossDqThreads, 1) cross_dq_tc_kernel(const _
         if (threadIdx.x == 0) report_abort(p.status, CQ_SMEM);
         return;
     }
+    next_may_start();
     if (threadIdx.x == 0) {
         s_abort = 0;
         // (a wait runs out a second after the launch at the earliest)

@@ -35,6 +35,7 @@ __global__ void __launch_bounds__(kFewThreads) cross_few_kernel(const CrossFewPa
     extern __shared__ __align__(16) uint8_t ring[];        // [stage][K, V][state][d]
     __shared__ float s_m[4][R], s_l[4][R], s_o[4][R][D];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, l8 = lane & 7, grp = lane >> 3;
+    next_may_start();
     if (blockIdx.x == 0 && threadIdx.x == 0) p.status[ST_STATUS] = p.status[ST_DETAIL] = 0;
     const int rank = blockIdx.x / p.Hkv, hk = blockIdx.x - rank * p.Hkv;
     const CrossFew it = p.items[rank];

@@ -61,6 +61,7 @@ __global__ void __launch_bounds__(kCrossThreads, 1) cross_fwd_tc_kernel(const __
     const uint32_t sQ = sbase, sK = sbase + 3 * TILE_BYTES, sV = sbase + 5 * TILE_BYTES;
     auto bar = [&](int i) { return smem_u32(&bars[i]); };
 
+    next_may_start();
     if (threadIdx.x == 0) {
         s_abort = 0;
         // (a wait runs out a second after the launch at the earliest)
