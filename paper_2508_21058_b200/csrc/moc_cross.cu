@@ -1,5 +1,5 @@
 // Cross attention to encoder states of another length (moc_cross_attend, moc_cross_attend_bwd): the plan, the entry points and the small
-// kernels that put shares together.  The attention itself: moc_cross_fwd_tc.cu, moc_cross_few.cu (few queries), moc_cross_dq_tc.cu, moc_cross_dkv_tc.cu.
+// kernels that put shares together.  The attention itself: moc_cross_fwd_tc.cu, moc_cross_solo_tc.cu (one query tile), moc_cross_few.cu (few queries), moc_cross_dq_tc.cu, moc_cross_dkv_tc.cu.
 #include <string.h>
 
 #include <algorithm>
@@ -30,29 +30,34 @@ static int check_cross(const moc_cross_problem *pr) {
 }
 
 // Shares of the keys.  With many items the longest-first walk balances the CTAs by itself; with few, and long key lists, an item is cut into
-// shares of `c` key tiles, whose results another launch puts together.  c is the one with the least estimated time, in key tiles of a
-// full item: the slowest CTA's walk, where an item costs 1.5 beside its tiles (its first loads and its results) and a tile 0.6 with a
-// single row tile, plus 3 for the second launch.
-static int share_tiles(const std::vector<CrossItem> &items, int H, int n_sm, int two_rows) {
-    int longest = 0;
-    for (const CrossItem &i : items) longest = std::max(longest, (i.n_keys + 127) / 128);
-    if (longest < 2 || items.size() * (size_t)H >= 4 * (size_t)n_sm) return std::max(longest, 1);
-    int best_c = longest;
-    double best = 1e300;
+// shares of `c` key tiles, whose results another launch puts together.  c is the one with the least estimated time `t`, in key tiles of
+// two-tile items (3450 cycles): the slowest CTA's walk, where an item costs 0.8 beside its tiles (2800: its first loads and its
+// results) and a key tile of a single query tile `single`, plus `join` for the second launch.
+struct Shares { int c; double t; };
+static Shares share_tiles(const std::vector<CrossItem> &items, int H, int n_sm, double single, double join) {
+    int longest = 1;
+    double total = 0;
+    for (const CrossItem &i : items) {
+        const int nt = (i.n_keys + 127) / 128;
+        longest = std::max(longest, nt);
+        if (nt > 0) total += 0.8 + (i.rows > 128 ? 1.0 : single) * nt;
+    }
+    if (items.size() * (size_t)H >= 4 * (size_t)n_sm) return Shares{longest, total * H / n_sm};
+    Shares best{longest, 1e300};
     std::vector<double> cost;
     for (int p = 1; p <= std::min(longest, 128); ++p) {
         const int c = (longest + p - 1) / p;
         cost.clear();
         for (const CrossItem &i : items) {
             const int nt = (i.n_keys + 127) / 128, n = std::max(1, (nt + c - 1) / c);
-            for (int x = 0; x < n; ++x) cost.push_back(1.5 + (i.rows > two_rows ? 1.0 : 0.6) * (nt * (x + 1) / n - nt * x / n));
+            for (int x = 0; x < n && nt > 0; ++x) cost.push_back(0.8 + (i.rows > 128 ? 1.0 : single) * ((int)((int64_t)nt * (x + 1) / n) - (int)((int64_t)nt * x / n)));
         }
         std::sort(cost.begin(), cost.end(), [](double a, double b) { return a > b; });
-        double t = c < longest ? 3.0 : 0.0;
+        double t = c < longest ? join : 0.0;
         for (size_t at = 0; at < cost.size() * (size_t)H; at += n_sm) t += cost[at / H];
-        if (t < best) { best = t; best_c = c; }
+        if (t < best.t) best = Shares{c, t};
     }
-    return best_c;
+    return best;
 }
 
 // cuts the items into shares of at most c key tiles; the longest items first
@@ -109,14 +114,47 @@ static void derive_cross(moc_cross *c, const moc_cross_problem *pr) {
         }
     }
     std::stable_sort(c->few.begin(), c->few.end(), [](const CrossFew &a, const CrossFew &b) { return a.n_keys > b.n_keys; });
+    // The forward's items: 256 rows, or a segment's last ones.  A key tile takes 3450 cycles for two query tiles; for a single one 4200 in
+    // the same kernel, 2100 in the one that has both softmax groups on one tile, which is a launch of its own.  So: all in the first
+    // kernel, or the single tiles in the second, or everything in tiles of 128 in the second, whichever is estimated shortest.
+    // (257 queries, 32k states, 24 heads: 188, 178 and 169 us; 576 queries, 77 states, 4 heads: 8.5 the first, 8.5 the last.)
+    std::vector<CrossItem> two, one, half, none;
     for (int s = 0; s < S; ++s) {
-        for (int q = pr->q_off[s]; !is_few(s) && q < pr->q_off[s + 1]; q += kCrossRows)
-            c->items.push_back(CrossItem{q, std::min(kCrossRows, pr->q_off[s + 1] - q), pr->k_off[s], keys(s), -1, {}});
-        for (int q = pr->q_off[s]; q < pr->q_off[s + 1]; q += 128)
-            c->dq_items.push_back(CrossItem{q, std::min(128, pr->q_off[s + 1] - q), pr->k_off[s], keys(s), -1, {}});
+        for (int q = pr->q_off[s]; !is_few(s) && q < pr->q_off[s + 1]; q += kCrossRows) {
+            const CrossItem i{q, std::min(kCrossRows, pr->q_off[s + 1] - q), pr->k_off[s], keys(s), -1, {}};
+            (i.n_keys == 0 ? none : i.rows <= 128 ? one : two).push_back(i);
+        }
+        for (int q = pr->q_off[s]; q < pr->q_off[s + 1]; q += 128) {
+            const CrossItem i{q, std::min(128, pr->q_off[s + 1] - q), pr->k_off[s], keys(s), -1, {}};
+            c->dq_items.push_back(i);
+            if (i.n_keys > 0 && !is_few(s)) half.push_back(i);
+        }
     }
-    cut_items(c->items, c->merges, c->prows, share_tiles(c->items, c->H, c->n_sm, 128));
-    cut_items(c->dq_items, c->dq_merges, c->dq_prows, share_tiles(c->dq_items, c->H, c->n_sm, 0));
+    std::vector<CrossItem> both = two;
+    both.insert(both.end(), one.begin(), one.end());
+    const double alone = 4200.0 / 3450.0, solo = 2100.0 / 3450.0, join = 3.5, launch = 1.5;
+    const Shares together = share_tiles(both, c->H, c->n_sm, alone, join), halves = share_tiles(half, c->H, c->n_sm, solo, join),
+                 pairs = share_tiles(two, c->H, c->n_sm, alone, join), singles = share_tiles(one, c->H, c->n_sm, solo, 0.5);
+    // (two launches, and K and V do not stay in L2 between them: 168 us and a merge of 10, where one launch of all tiles takes 162 and 7)
+    int64_t states = 0;
+    for (int s = 0; s < S; ++s) states += keys(s);
+    const bool in_l2 = states * c->Hkv * c->d * 4 <= (96ll << 20);
+    const double apart = two.empty() || one.empty() || !in_l2 ? 1e300 : pairs.t + singles.t + launch;
+    Shares cut = together;
+    if (halves.t < std::min(together.t, apart)) {
+        c->solo.swap(half);
+        cut_items(c->solo, c->merges, c->prows, halves.c);
+    } else if (apart < together.t) {
+        c->items.swap(two);
+        c->solo.swap(one);
+        cut_items(c->solo, c->merges, c->prows, singles.c);
+        cut = pairs;
+    } else {
+        c->items.swap(both);
+    }
+    c->items.insert(c->items.end(), none.begin(), none.end());
+    cut_items(c->items, c->merges, c->prows, cut.c);
+    cut_items(c->dq_items, c->dq_merges, c->dq_prows, share_tiles(c->dq_items, c->H, c->n_sm, 1.0, 3.0).c);
     for (const CrossMerge &m : c->merges) c->most_merge_rows = std::max(c->most_merge_rows, m.rows);
     for (const CrossItem &i : c->items) c->n_work += i.n_keys > 0;
     for (const CrossItem &i : c->dq_items) c->n_dq_work += i.n_keys > 0;
@@ -307,11 +345,12 @@ extern "C" int moc_cross_create(const moc_cross_problem *pr, moc_cross **out) {
         auto take = [&](size_t bytes) { const size_t at = o; o = up256(o + bytes); return at; };
         const size_t a = take(sizeof(CrossItem) * c->items.size()), b = take(sizeof(CrossItem) * c->dq_items.size()),
                      m = take(sizeof(CrossMerge) * c->merges.size()), dm = take(sizeof(CrossMerge) * c->dq_merges.size()),
-                     fe = take(sizeof(CrossFew) * c->few.size()), p = take(sizeof(CrossPiece) * c->pieces.size()), po = take(4 * c->piece_off.size()), su = take(sizeof(CrossSum) * c->sums.size());
+                     fe = take(sizeof(CrossFew) * c->few.size()), so = take(sizeof(CrossItem) * c->solo.size()), p = take(sizeof(CrossPiece) * c->pieces.size()), po = take(4 * c->piece_off.size()), su = take(sizeof(CrossSum) * c->sums.size());
         std::vector<char> host(o);
         auto up = [&](size_t at, const void *src, size_t bytes) { if (bytes) memcpy(host.data() + at, src, bytes); };
         up(a, c->items.data(), sizeof(CrossItem) * c->items.size());
         up(b, c->dq_items.data(), sizeof(CrossItem) * c->dq_items.size());
+        up(so, c->solo.data(), sizeof(CrossItem) * c->solo.size());
         up(fe, c->few.data(), sizeof(CrossFew) * c->few.size());
         up(m, c->merges.data(), sizeof(CrossMerge) * c->merges.size());
         up(dm, c->dq_merges.data(), sizeof(CrossMerge) * c->dq_merges.size());
@@ -337,7 +376,7 @@ extern "C" int moc_cross_create(const moc_cross_problem *pr, moc_cross **out) {
             return MOC_ERR_CUDA;
         }
         char *d = static_cast<char *>(c->d_blob);
-        c->d_items = (CrossItem *)(d + a); c->d_dq_items = (CrossItem *)(d + b); c->d_few = (CrossFew *)(d + fe);
+        c->d_items = (CrossItem *)(d + a); c->d_dq_items = (CrossItem *)(d + b); c->d_few = (CrossFew *)(d + fe); c->d_solo = (CrossItem *)(d + so);
         c->d_merges = (CrossMerge *)(d + m); c->d_dq_merges = (CrossMerge *)(d + dm);
         c->d_pieces = (CrossPiece *)(d + p); c->d_piece_off = (int32_t *)(d + po); c->d_sums = (CrossSum *)(d + su);
     } catch (...) {
@@ -377,6 +416,8 @@ extern "C" int moc_cross_attend(const moc_cross *c, const moc_rows *Q, const moc
     }
     if (!c->few.empty())
         if (int r = launch_cross_few(c, Q, K, V, O, lse, ws, s)) return r;
+    if (!c->solo.empty())
+        if (int r = launch_cross_solo(c, Q, K, V, O, lse, ws, s)) return r;
     if (!c->items.empty())
         if (int r = launch_cross_fwd(c, Q, K, V, O, lse, ws, s)) return r;
     if (!c->merges.empty()) {

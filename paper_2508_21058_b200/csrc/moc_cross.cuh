@@ -38,7 +38,7 @@ struct CrossLayout {
 struct moc_cross {
     int H, Hkv, g, d, Lq, Lk, device, n_sm;
     float scale;
-    std::vector<moc::CrossItem> items, dq_items;       // per head, the longest first
+    std::vector<moc::CrossItem> items, solo, dq_items; // per head, the longest first; solo: items of one query tile with a launch of their own
     std::vector<moc::CrossMerge> merges, dq_merges;    // per head
     std::vector<moc::CrossPiece> pieces;
     std::vector<int32_t> piece_off;                    // of every CTA of the key-stationary pass
@@ -49,7 +49,7 @@ struct moc_cross {
     int prows = 0, dq_prows = 0, kv_slots = 0;         // rows of partial results of a head, the same of dQ; slots in all
     int n_work = 0, n_dq_work = 0;                     // items that have keys: the others, which come last, only need zeros
     void *d_blob = nullptr;
-    moc::CrossItem *d_items, *d_dq_items;
+    moc::CrossItem *d_items, *d_solo, *d_dq_items;
     moc::CrossFew *d_few;
     moc::CrossMerge *d_merges, *d_dq_merges;
     moc::CrossPiece *d_pieces;
@@ -85,6 +85,8 @@ __device__ __forceinline__ int cross_items(int n_all) {
 __device__ __forceinline__ void prefetch_item(const CrossItem *item) { asm volatile("prefetch.global.L1 [%0];" ::"l"(item)); }
 #endif
 
+int launch_cross_solo(const moc_cross *c, const moc_rows *Q, const moc_rows *K, const moc_rows *V, const moc_rows *O, float *lse, void *ws,
+                      cudaStream_t s);
 int launch_cross_few(const moc_cross *c, const moc_rows *Q, const moc_rows *K, const moc_rows *V, const moc_rows *O, float *lse, void *ws,
                      cudaStream_t s);
 int launch_cross_fwd(const moc_cross *c, const moc_rows *Q, const moc_rows *K, const moc_rows *V, const moc_rows *O, float *lse, void *ws,

@@ -32,6 +32,12 @@ CASES = [
     (4, 2, 64, [3, 0, 1], [1000, 9, 31], 2),
     (5, 5, 128, [1], [4097], 0),
     (7, 1, 128, [1, 1], [33, 640], 0),
+    # one query tile an item: both softmax groups on it, an odd and an even number of key tiles, shares, beside two-tile items
+    (3, 1, 128, [100, 128, 9], [1000, 129, 128], 2),
+    (2, 2, 64, [64], [5000], 0),
+    (24, 8, 128, [50] * 6, [300, 17, 500, 256, 1, 384], 1),
+    (32, 32, 64, [257], [12000], 0),
+    (40, 40, 128, [384, 0, 90], [8000, 4, 3000], 1),
 ]
 
 
