@@ -121,6 +121,7 @@ namespace moc {
 
 extern std::atomic<long long> g_launches;
 void set_cuda_error(cudaError_t e, const char *where);
+cudaError_t table_stream(cudaStream_t *out);       // the stream on which plans' tables are made (moc_plan.cu)
 
 #define MOC_CUDA_TRY(expr)                                         \
     do {                                                           \

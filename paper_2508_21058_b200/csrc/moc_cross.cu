@@ -33,6 +33,8 @@ static int check_cross(const moc_cross_problem *pr) {
 // shares of `c` key tiles, whose results another launch puts together.  c is the one with the least estimated time `t`, in key tiles of
 // two-tile items (3450 cycles): the slowest CTA's walk, where an item costs 0.8 beside its tiles (2800: its first loads and its
 // results) and a key tile of a single query tile `single`, plus `join` for the second launch.
+// (No share has more than 16384 key tiles, some 50 ms: a bounded wait lasts a second.)
+constexpr int kMostTiles = 16384;
 struct Shares { int c; double t; };
 static Shares share_tiles(const std::vector<CrossItem> &items, int H, int n_sm, double single, double join) {
     int longest = 1;
@@ -42,7 +44,7 @@ static Shares share_tiles(const std::vector<CrossItem> &items, int H, int n_sm, 
         longest = std::max(longest, nt);
         if (nt > 0) total += 0.8 + (i.rows > 128 ? 1.0 : single) * nt;
     }
-    if (items.size() * (size_t)H >= 4 * (size_t)n_sm) return Shares{longest, total * H / n_sm};
+    if (items.size() * (size_t)H >= 4 * (size_t)n_sm) return Shares{std::min(longest, kMostTiles), total * H / n_sm};
     Shares best{longest, 1e300};
     std::vector<double> cost;
     for (int p = 1; p <= std::min(longest, 128); ++p) {
@@ -56,7 +58,9 @@ static Shares share_tiles(const std::vector<CrossItem> &items, int H, int n_sm, 
         double t = c < longest ? join : 0.0;
         for (size_t at = 0; at < cost.size() * (size_t)H; at += n_sm) t += cost[at / H];
         if (t < best.t) best = Shares{c, t};
+        if (cost.size() * (size_t)H > 4 * (size_t)n_sm) break;   // (shorter shares only cost more)
     }
+    best.c = std::min(best.c, kMostTiles);
     return best;
 }
 
@@ -194,6 +198,7 @@ static void derive_cross(moc_cross *c, const moc_cross_problem *pr) {
         if (t < best) { best = t; part = len; }
         if (at > 64ll * c->n_sm) break;                              // (shorter parts only cost more)
     }
+    part = std::min<int64_t>(part, 1 << 16);                         // (a bounded wait lasts a second, as long as 500000 pairs)
     std::vector<CrossPiece> all;
     for (const Group &g : groups) {
         const int64_t parts = (g.units + part - 1) / part;
@@ -361,13 +366,9 @@ extern "C" int moc_cross_create(const moc_cross_problem *pr, moc_cross **out) {
         if (e == cudaSuccess) {
             // on a stream of its own: on the legacy stream the copy would wait for what the caller has under way there
             cudaStream_t st = nullptr;
-            e = cudaStreamCreateWithFlags(&st, cudaStreamNonBlocking);
-            if (e == cudaSuccess) {
-                e = cudaMemcpyAsync(c->d_blob, host.data(), o, cudaMemcpyHostToDevice, st);
-                const cudaError_t e2 = cudaStreamSynchronize(st);
-                cudaStreamDestroy(st);
-                if (e == cudaSuccess) e = e2;
-            }
+            e = table_stream(&st);
+            if (e == cudaSuccess) e = cudaMemcpyAsync(c->d_blob, host.data(), o, cudaMemcpyHostToDevice, st);
+            if (e == cudaSuccess) e = cudaStreamSynchronize(st);
         }
         if (e != cudaSuccess) {
             set_cuda_error(e, "cross attention tables");
@@ -414,12 +415,13 @@ extern "C" int moc_cross_attend(const moc_cross *c, const moc_rows *Q, const moc
         MOC_CUDA_TRY(cudaMemsetAsync(ws_ptr<int>(ws, c->ws.status), 0, 8, s));
         return MOC_OK;
     }
+    // (the first of them clears the status)
     if (!c->few.empty())
         if (int r = launch_cross_few(c, Q, K, V, O, lse, ws, s)) return r;
     if (!c->solo.empty())
-        if (int r = launch_cross_solo(c, Q, K, V, O, lse, ws, s)) return r;
+        if (int r = launch_cross_solo(c, Q, K, V, O, lse, ws, c->few.empty(), s)) return r;
     if (!c->items.empty())
-        if (int r = launch_cross_fwd(c, Q, K, V, O, lse, ws, s)) return r;
+        if (int r = launch_cross_fwd(c, Q, K, V, O, lse, ws, c->few.empty() && c->solo.empty(), s)) return r;
     if (!c->merges.empty()) {
         const dim3 grid((unsigned)c->merges.size(), c->H, (c->most_merge_rows + 7) / 8);
         const float *po = ws_ptr<float>(ws, c->ws.part_o), *pl = ws_ptr<float>(ws, c->ws.part_lse);

@@ -85,12 +85,10 @@ __device__ __forceinline__ int cross_items(int n_all) {
 __device__ __forceinline__ void prefetch_item(const CrossItem *item) { asm volatile("prefetch.global.L1 [%0];" ::"l"(item)); }
 #endif
 
-int launch_cross_solo(const moc_cross *c, const moc_rows *Q, const moc_rows *K, const moc_rows *V, const moc_rows *O, float *lse, void *ws,
-                      cudaStream_t s);
+int launch_cross_solo(const moc_cross *c, const moc_rows *Q, const moc_rows *K, const moc_rows *V, const moc_rows *O, float *lse, void *ws, bool first, cudaStream_t s);
 int launch_cross_few(const moc_cross *c, const moc_rows *Q, const moc_rows *K, const moc_rows *V, const moc_rows *O, float *lse, void *ws,
                      cudaStream_t s);
-int launch_cross_fwd(const moc_cross *c, const moc_rows *Q, const moc_rows *K, const moc_rows *V, const moc_rows *O, float *lse, void *ws,
-                     cudaStream_t s);
+int launch_cross_fwd(const moc_cross *c, const moc_rows *Q, const moc_rows *K, const moc_rows *V, const moc_rows *O, float *lse, void *ws, bool first, cudaStream_t s);
 // (also writes delta)
 int launch_cross_dq(const moc_cross *c, const moc_rows *Q, const moc_rows *K, const moc_rows *V, const moc_rows *O, const float *lse, const moc_rows *dO,
                     const moc_rows *dQ, void *ws, cudaStream_t s);

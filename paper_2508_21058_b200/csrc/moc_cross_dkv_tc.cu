@@ -33,7 +33,7 @@ struct CrossKvParams {
     WaitBound wait;
 };
 
-enum CrossKvWait { CB_XFULL = 64, CB_YFULL, CB_YEMPTY, CB_T1FULL, CB_T2FULL, CB_PDONE, CB_DSDONE, CB_ACCFULL, CB_ACCFREE, CB_SMEM };
+enum CrossKvWait { CB_XFULL = 64, CB_YFULL, CB_YEMPTY, CB_T1FULL, CB_T2FULL, CB_PDONE, CB_DSDONE, CB_ACCFULL, CB_SMEM };
 
 constexpr int kCrossY1 = 3, kCrossY2 = 2;      // stages of the streamed tiles Q (read twice per tile) and dO
 constexpr int kCrossKvThreads = 512;
@@ -48,7 +48,7 @@ __global__ void __launch_bounds__(kCrossKvThreads, 1) cross_dkv_tc_kernel(const 
     constexpr int CH = D / 8;               // 16-byte pieces per row
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     enum { X_FULL = 0, Y1_FULL = 1, Y1_EMPTY = 4, Y2_FULL = 7, Y2_EMPTY = 9, T1_FULL = 11, T2_FULL = 13, P_HALF = 15, P_DONE = 16, DS_DONE = 17,
-           ACC_FULL = 19, T1_ISSUED = 20, ACC_FREE = 22, N_BARS = 23 };
+           ACC_FULL = 19, T1_ISSUED = 20, N_BARS = 22 };
     __shared__ __align__(8) uint64_t bars[N_BARS];
     __shared__ uint32_t tmem_slot;
     __shared__ int s_abort;
@@ -71,7 +71,7 @@ __global__ void __launch_bounds__(kCrossKvThreads, 1) cross_dkv_tc_kernel(const 
         s_abort = 0;
         for (int b = 0; b < N_BARS; ++b)
             mbar_init(bar(b), (b >= Y1_FULL && b < Y1_EMPTY) || (b >= Y2_FULL && b < T1_FULL) || b == ACC_FULL ? 2      // two warps, or both issuers
-                              : (b >= P_HALF && b < ACC_FULL) || b == ACC_FREE ? 256 : 1);
+                              : b >= P_HALF && b < ACC_FULL ? 256 : 1);
         fence_barrier_init();
     }
     __syncthreads();
@@ -189,10 +189,7 @@ __global__ void __launch_bounds__(kCrossKvThreads, 1) cross_dkv_tc_kernel(const 
                 for (int x = 0; x < NJ / 2; ++x)
                     tmem_ld_16x256b(tmem + lane_off + 256 + side * 128 + ((uint32_t)(x + (j0 >> 1)) << 20) + cb * 64, v[x]);
                 tmem_wait_ld();
-                if (side == 1) {
-                    tc_fence_before();
-                    mbar_arrive(bar(ACC_FREE));              // the next piece's sums may begin
-                }
+                tc_fence_before();                           // (before this thread's next P, which the next piece's sums wait for)
                 const float w = side ? 1.f : p.scale;
                 const CrossRows &out = side ? p.dV : p.dK;
 #pragma unroll
@@ -388,7 +385,6 @@ __global__ void __launch_bounds__(kCrossKvThreads, 1) cross_dkv_tc_kernel(const 
                     for (; ok && j < j0 + n_tiles; ++j) {
                         const bool more = j + 1 < j0 + n_tiles;
                         wait(Y2_FULL + (j & 1), (j >> 1) & 1, CB_YFULL);
-                        if (j == j0 && pn > 0) wait(ACC_FREE, (pn - 1) & 1, CB_ACCFREE);
                         wait(P_HALF, j & 1, CB_PDONE);
                         if (!ok) break;
                         tc_fence_after();
@@ -428,7 +424,6 @@ __global__ void __launch_bounds__(kCrossKvThreads, 1) cross_dkv_tc_kernel(const 
                         }
                         wait(Y1_FULL + s3, ph3, CB_YFULL);                     // (long there: dS(j) follows T1(j))
                         wait(DS_DONE + (j & 1), (j >> 1) & 1, CB_DSDONE);
-                        if (j == j0 && pn > 0) wait(ACC_FREE, (pn - 1) & 1, CB_ACCFREE);
                         if (!ok) break;
                         tc_fence_after();
                         acc1(s3, j > j0);

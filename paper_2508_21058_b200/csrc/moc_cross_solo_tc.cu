@@ -23,6 +23,7 @@ struct CrossSoloParams {
     CrossRows V, O;
     float *lse, *part_o, *part_lse;
     int *status;
+    int first;                         // the call's first launch clears the status
     float scale_log2;
     WaitBound wait;
 };
@@ -59,7 +60,7 @@ __global__ void __launch_bounds__(kCrossSoloThreads, 1) cross_solo_tc_kernel(con
     if (threadIdx.x == 0) {
         s_abort = 0;
         // (a wait runs out a second after the launch at the earliest)
-        if (blockIdx.x == 0) p.status[ST_STATUS] = p.status[ST_DETAIL] = 0;
+        if (p.first && blockIdx.x == 0) p.status[ST_STATUS] = p.status[ST_DETAIL] = 0;
         for (int t = 0; t < 3; ++t) {
             mbar_init(bar(Q_FULL + t), 1);
             mbar_init(bar(Q_EMPTY + t), 2);            // both issuers: each sees every phase of Q_FULL
@@ -424,7 +425,7 @@ __global__ void __launch_bounds__(kCrossSoloThreads, 1) cross_solo_tc_kernel(con
 
 template <int D>
 static int cross_solo_d(const moc_cross *c, const moc_rows *Q, const moc_rows *K, const moc_rows *V, const moc_rows *O, float *lse, void *ws,
-                        cudaStream_t s) {
+                        bool first, cudaStream_t s) {
     CUtensorMap tmQ, tmK, tmV, tmK16, tmV16;
     if (int r = make_tmap_rows_bf16(&tmQ, Q, c->H, c->Lq, D, 128)) return r;
     if (int r = make_tmap_rows_bf16(&tmK, K, c->Hkv, c->Lk, D, 128)) return r;
@@ -436,7 +437,7 @@ static int cross_solo_d(const moc_cross *c, const moc_rows *Q, const moc_rows *K
     a.H = c->H; a.g = c->g; a.Lq = c->Lq; a.prows = c->prows;
     a.V = CrossRows(V); a.O = CrossRows(O); a.lse = lse;
     a.part_o = ws_ptr<float>(ws, c->ws.part_o); a.part_lse = ws_ptr<float>(ws, c->ws.part_lse);
-    a.status = ws_ptr<int>(ws, c->ws.status);
+    a.status = ws_ptr<int>(ws, c->ws.status); a.first = first;
     a.scale_log2 = c->scale * 1.4426950408889634f;
     a.wait = WaitBound::of(0);
     // always the d = 128 footprint: more than half an SM's shared memory, so that CTAs, which each take all of the tensor memory, never share one
@@ -448,8 +449,8 @@ static int cross_solo_d(const moc_cross *c, const moc_rows *Q, const moc_rows *K
 }
 
 int launch_cross_solo(const moc_cross *c, const moc_rows *Q, const moc_rows *K, const moc_rows *V, const moc_rows *O, float *lse, void *ws,
-                      cudaStream_t s) {
-    return c->d == 128 ? cross_solo_d<128>(c, Q, K, V, O, lse, ws, s) : cross_solo_d<64>(c, Q, K, V, O, lse, ws, s);
+                      bool first, cudaStream_t s) {
+    return c->d == 128 ? cross_solo_d<128>(c, Q, K, V, O, lse, ws, first, s) : cross_solo_d<64>(c, Q, K, V, O, lse, ws, first, s);
 }
 
 }  // namespace moc

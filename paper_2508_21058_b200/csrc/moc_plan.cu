@@ -50,7 +50,7 @@ __global__ void token_chunk_kernel(const int32_t *__restrict__ off, int32_t *__r
 
 // The stream on which plans get their tables, one per context for as long as the process lives (making one takes 100 us).  A stream
 // belongs to the context it was made in, and a device can have several, or a new one after cudaDeviceReset.
-static cudaError_t table_stream(cudaStream_t *out) {
+cudaError_t table_stream(cudaStream_t *out) {
     typedef CUresult (*CtxGetIdFn)(CUcontext, unsigned long long *);
     struct Entry { unsigned long long ctx; cudaStream_t stream; };
     static std::mutex mu;
