@@ -272,6 +272,7 @@ int moc_rope_workspace_bytes(const moc_rope *rope, size_t *bytes);     /* for mo
  * x_type (MOC_BF16, MOC_FP32) is the type of q and k; q_out, k_out are bf16, in the layout that moc_chunk_pool / moc_route /
  * moc_attend take when they are contiguous [H][L][d].  w_q, w_k: DEVICE fp32 [d], shared by all heads.  pos: DEVICE int32
  * [n_tokens][n_axes] (any value; angles are formed in 64 bits).  n_k_heads may be 0: k, w_k, k_out are not looked at then.  n_tokens may be 0.
+ * Squares are summed in fp32: rows of values beyond 1e18, or without an eps below 1e-19, leave its range.
  * An output may be its own input where type and strides are the same; no other overlap. */
 int moc_norm_rope(const moc_rope *rope, int x_type, int32_t n_tokens, int32_t n_q_heads, int32_t n_k_heads, const int32_t *pos,
                   const moc_rows *q, const float *w_q, const moc_rows *q_out, const moc_rows *k, const float *w_k,
@@ -310,7 +311,8 @@ int moc_cross_workspace_bytes(const moc_cross *cross, int with_bwd, size_t *byte
 /* O = softmax(scale Q K^T) V over the segment's states, lse (fp32, [n_heads][q_off[n_segments]] contiguous) = ln of the sum of
  * exp(scale q.k).  Q, O: bf16 rows of n_heads heads and q_off[n_segments] tokens (at least: rows behind them are neither read nor written);
  * K, V: of n_kv_heads heads and k_off[n_segments] tokens.  A query without states gets O = 0 and lse = -inf.  Padding is
- * not looked at: it may hold anything.  Products in bf16, fp32 accumulation and softmax. */
+ * not looked at: it may hold anything.  Products in bf16, fp32 accumulation and softmax (segments of up to eight rows of
+ * the query heads that share a key head: fp32 throughout).  No tensor may overlap one that is written. */
 int moc_cross_attend(const moc_cross *cross, const moc_rows *Q, const moc_rows *K, const moc_rows *V, const moc_rows *O, float *lse,
                      void *ws, void *stream);
 

@@ -95,11 +95,26 @@ static void derive_cross(moc_cross *c, const moc_cross_problem *pr) {
         const int n = pr->q_off[s + 1] - pr->q_off[s];
         return n > 0 && (int64_t)n * c->g <= kFewRows && keys(s) > 0;
     };
-    // Few queries: shares of the states so that there are eight blocks for every SM (two to four are resident), of 128 states at least.
-    int64_t few_keys = 0;
+    // Few queries: shares of the states, of 128 at least.  Three blocks are resident on an SM.  Either no more shares than that, all under
+    // way at once, the launch as long as the longest; or four for every SM, the longest first, the launch about the mean and one
+    // more share long.  (1 head, 1M states: 108 us and 136; 64 sequences of 375 to 1500, 24 heads on 8, which no single wave
+    // takes in equal parts: 65 and 56; six and eight for every SM 58 and 63.)
+    int64_t few_work = 0, few_longest = 0;
+    auto few_blocks = [&](int s) { return ((pr->q_off[s + 1] - pr->q_off[s]) * c->g + 3) / 4; };
     for (int s = 0; s < S; ++s)
-        if (is_few(s)) few_keys += (int64_t)keys(s) * c->Hkv;
-    const int64_t few_share = std::max<int64_t>(128, (few_keys / (8 * c->n_sm) + 31) / 32 * 32);
+        if (is_few(s)) {
+            few_work += (int64_t)keys(s) * c->Hkv * few_blocks(s);
+            few_longest = std::max<int64_t>(few_longest, keys(s));
+        }
+    const int64_t slots = 3 * (int64_t)c->n_sm, mean = few_work / slots;
+    auto round_share = [](int64_t n) { return std::max<int64_t>(128, (n + 31) / 32 * 32); };
+    int64_t few_share = round_share(few_work / (4 * (int64_t)c->n_sm));
+    for (int64_t one = round_share(mean); few_work > 0 && one < 2 * few_longest + 128 && one <= mean + few_share; one = round_share(one + one / 16 + 1)) {
+        int64_t n = 0;
+        for (int s = 0; s < S; ++s)
+            if (is_few(s)) n += (keys(s) + one - 1) / one * c->Hkv * few_blocks(s);
+        if (n <= slots) { few_share = one; break; }
+    }
     for (int s = 0; s < S; ++s) {
         if (!is_few(s)) continue;
         const int q_len = pr->q_off[s + 1] - pr->q_off[s], rows = q_len * c->g, blocks = (rows + 3) / 4, nk = keys(s);
@@ -159,7 +174,10 @@ static void derive_cross(moc_cross *c, const moc_cross_problem *pr) {
     c->items.insert(c->items.end(), none.begin(), none.end());
     cut_items(c->items, c->merges, c->prows, cut.c);
     cut_items(c->dq_items, c->dq_merges, c->dq_prows, share_tiles(c->dq_items, c->H, c->n_sm, 1.0, 3.0).c);
-    for (const CrossMerge &m : c->merges) c->most_merge_rows = std::max(c->most_merge_rows, m.rows);
+    for (const CrossMerge &m : c->merges) {
+        c->most_merge_rows = std::max(c->most_merge_rows, m.rows);
+        c->most_merge_n = std::max(c->most_merge_n, m.n);
+    }
     for (const CrossItem &i : c->items) c->n_work += i.n_keys > 0;
     for (const CrossItem &i : c->dq_items) c->n_dq_work += i.n_keys > 0;
 
@@ -246,34 +264,36 @@ static cudaError_t launch_after(void (*kernel)(P...), dim3 grid, cudaStream_t s,
     return cudaLaunchKernelEx(&c, kernel, std::forward<A>(args)...);
 }
 
-// ---- shares of the forward: O = sum_i w_i O_i / sum_i w_i, w_i = exp(lse_i - max lse); a warp a row, four shares' loads under way
-template <int D>
+// ---- shares of the forward: O = sum_i w_i O_i / sum_i w_i, w_i = exp(lse_i - max lse), four shares' loads under way.  A warp has a row, or,
+// WIDE, the eight warps of a block have one and every eighth share each.
+template <int D, bool WIDE>
 __global__ void __launch_bounds__(256) cross_merge_kernel(const CrossMerge *merges, const float *part_o, const float *part_lse, int prows,
                                                           CrossRows O, float *lse, int Lq) {
+    constexpr int V = D / 32, W = WIDE ? 8 : 1;                // channels of a lane, warps of a row
+    __shared__ float s_o[WIDE ? 8 : 1][D], s_sum[8];
     const CrossMerge m = merges[blockIdx.x];
-    const int h = blockIdx.y, row = blockIdx.z * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, h = blockIdx.y, row = WIDE ? blockIdx.z : blockIdx.z * 8 + warp;
     previous_done();
-    if (row >= m.rows) return;
+    if (row >= m.rows) return;                                 // (WIDE: the whole block)
     const size_t at = (size_t)h * prows + m.slot + row;
     float big = -INFINITY;
     for (int i = lane; i < m.n; i += 32) big = fmaxf(big, part_lse[at + (size_t)i * m.rows]);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, o));
-    constexpr int V = D / 32;
     float acc[V] = {}, sum = 0.f;
-    for (int i = 0; i < m.n; i += 4) {
+    for (int i = WIDE ? warp : 0; i < m.n; i += 4 * W) {
         float2 v[4][V / 2];
         float w[4];
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
-            const size_t src = at + (size_t)min(i + x, m.n - 1) * m.rows;
+            const size_t src = at + (size_t)min(i + x * W, m.n - 1) * m.rows;
             w[x] = part_lse[src];
 #pragma unroll
             for (int y = 0; y < V / 2; ++y) v[x][y] = *reinterpret_cast<const float2 *>(part_o + src * D + lane * V + 2 * y);
         }
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
-            if (i + x >= m.n) break;
+            if (i + x * W >= m.n) break;
             const float e = __expf(w[x] - big);
             sum += e;
 #pragma unroll
@@ -281,6 +301,22 @@ __global__ void __launch_bounds__(256) cross_merge_kernel(const CrossMerge *merg
                 acc[2 * y] = fmaf(e, v[x][y].x, acc[2 * y]);
                 acc[2 * y + 1] = fmaf(e, v[x][y].y, acc[2 * y + 1]);
             }
+        }
+    }
+    if constexpr (WIDE) {                                      // in the order of the warps
+        if (lane == 0) s_sum[warp] = sum;
+#pragma unroll
+        for (int y = 0; y < V; ++y) s_o[warp][lane * V + y] = acc[y];
+        __syncthreads();
+        if (warp > 0) return;
+        sum = 0.f;
+#pragma unroll
+        for (int y = 0; y < V; ++y) acc[y] = 0.f;
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+            sum += s_sum[x];
+#pragma unroll
+            for (int y = 0; y < V; ++y) acc[y] += s_o[x][lane * V + y];
         }
     }
     const float inv = 1.f / sum;
@@ -423,10 +459,12 @@ extern "C" int moc_cross_attend(const moc_cross *c, const moc_rows *Q, const moc
     if (!c->items.empty())
         if (int r = launch_cross_fwd(c, Q, K, V, O, lse, ws, c->few.empty() && c->solo.empty(), s)) return r;
     if (!c->merges.empty()) {
-        const dim3 grid((unsigned)c->merges.size(), c->H, (c->most_merge_rows + 7) / 8);
+        const bool wide = c->most_merge_n > 16;
+        const dim3 grid((unsigned)c->merges.size(), c->H, wide ? c->most_merge_rows : (c->most_merge_rows + 7) / 8);
         const float *po = ws_ptr<float>(ws, c->ws.part_o), *pl = ws_ptr<float>(ws, c->ws.part_lse);
-        MOC_CUDA_TRY(launch_after(c->d == 128 ? cross_merge_kernel<128> : cross_merge_kernel<64>, grid, s, (const CrossMerge *)c->d_merges, po, pl, c->prows,
-                                  CrossRows(O), lse, c->Lq));
+        auto kernel = c->d == 128 ? (wide ? cross_merge_kernel<128, true> : cross_merge_kernel<128, false>)
+                                  : (wide ? cross_merge_kernel<64, true> : cross_merge_kernel<64, false>);
+        MOC_CUDA_TRY(launch_after(kernel, grid, s, (const CrossMerge *)c->d_merges, po, pl, c->prows, CrossRows(O), lse, c->Lq));
         MOC_LAUNCH_CHECK();
     }
     return MOC_OK;

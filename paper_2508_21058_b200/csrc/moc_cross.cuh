@@ -45,7 +45,7 @@ struct moc_cross {
     std::vector<moc::CrossSum> sums;
     std::vector<moc::CrossFew> few;                    // per key head, the longest first
     int few_rows = 0;                                  // the most rows that one has
-    int most_merge_rows = 0;                           // of the forward's merges
+    int most_merge_rows = 0, most_merge_n = 0;         // of the forward's merges
     int prows = 0, dq_prows = 0, kv_slots = 0;         // rows of partial results of a head, the same of dQ; slots in all
     int n_work = 0, n_dq_work = 0;                     // items that have keys: the others, which come last, only need zeros
     void *d_blob = nullptr;

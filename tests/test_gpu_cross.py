@@ -32,6 +32,8 @@ CASES = [
     (4, 2, 64, [3, 0, 1], [1000, 9, 31], 2),
     (5, 5, 128, [1], [4097], 0),
     (7, 1, 128, [1, 1], [33, 640], 0),
+    (1, 1, 128, [2], [20000], 0),                       # more shares than a warp puts together
+    (1, 1, 64, [130, 3], [9000, 4000], 0),
     # one query tile an item: both softmax groups on it, an odd and an even number of key tiles, shares, beside two-tile items
     (3, 1, 128, [100, 128, 9], [1000, 129, 128], 2),
     (2, 2, 64, [64], [5000], 0),
