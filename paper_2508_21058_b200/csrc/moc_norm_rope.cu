@@ -280,6 +280,7 @@ __global__ void __launch_bounds__(kRopeWarps * 32, RopeBatch<X, BWD>::BLOCKS) no
                 }
 #pragma unroll
                 for (int y = 0; y < U; ++y) {
+                    if (y > 0 && y * RPW >= left + sub) break;      // (no lane has such a row)
                     Pairs v = rx[y].template get<HALVES>();
                     uint64_t r2 = 0;
                     if (norm) {

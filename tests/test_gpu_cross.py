@@ -160,6 +160,23 @@ def test_nothing_to_attend(q_len, k_len):
     assert bool((run.dk[:, :run.Lk] == 0).all()) and bool((run.dv[:, :run.Lk] == 0).all()) and bool((run.dk[:, run.Lk:] == 7.0).all())
 
 
+@pytest.mark.parametrize("q_len,k_len", [([], []), ([0, 0], [5, 0]), ([4, 2], [0, 0]), ([300, 2], [0, 40])])
+def test_nothing_to_attend_in_a_graph(q_len, k_len):
+    run = Run((2, 1, 64, q_len, k_len, 1), seed=17)
+    run.forward().backward()
+    torch.cuda.synchronize()
+    want = [t.clone() for t in run.outputs()]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run.forward().backward()
+    for t in run.outputs():
+        t.fill_(3.0)
+    graph.replay()
+    torch.cuda.synchronize()
+    for a, b, n in zip(run.outputs(), want, (run.Lq, run.Lq, run.Lq, run.Lk, run.Lk)):
+        assert torch.equal(a[:, :n], b[:, :n])
+
+
 def test_a_bad_value_stays_with_those_who_see_it():
     """An infinite value in one segment's states, NaN in one query and its gradient: other segments' results are as without them."""
     clean = Run((2, 1, 128, [100, 60, 40], [90, 50, 300], 0), seed=8).forward().backward()
