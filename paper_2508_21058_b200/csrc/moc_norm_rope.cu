@@ -207,12 +207,14 @@ __device__ __forceinline__ float row_sum(float v) {
     return v;
 }
 
-// Rows of a lane under way, and blocks per SM: what the registers hold.  (Backward, bf16, 33k tokens of 24 + 24 heads and 6.4k of 12 + 4 at
-// d = 64: four rows and two blocks 234 and 23.1 us, three and three 230 and 21.4, two and three 239 and 21.4, two and four 280 and 28.)
+// Rows of a lane under way, and blocks per SM: what the registers hold.  (33k tokens of 24 + 24 heads, bf16: forward, six rows and three
+// blocks 131 us, four and three 136, eight and two 152, four and four 136; backward, six and two 218, three and three 231,
+// four and three 240, five and two 240, eight and two 235.  An fp32 projection, 12.8k tokens of 24 + 8 heads, forward: four and three
+// 50, six and two 56, eight and two 58; backward, four and two 85, three 91, six 102.)
 template <typename X, bool BWD>
 struct RopeBatch {
-    static constexpr int U = !BWD ? 4 : sizeof(X) == 4 ? 2 : 3;
-    static constexpr int BLOCKS = BWD && sizeof(X) == 4 ? 2 : 3;
+    static constexpr int U = sizeof(X) == 4 ? 4 : 6;
+    static constexpr int BLOCKS = BWD ? 2 : 3;
 };
 
 // FULL: every channel is turned
