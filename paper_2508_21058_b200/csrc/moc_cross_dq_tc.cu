@@ -15,6 +15,8 @@
 //   warps 10, 11, 14, 15  its delta, 32 rows each;
 //   warps 12,13 MMA issuers: warp 12 T1, warp 13 T2 and ACC.  T1(j + 1) is issued once the lanes have read T1(j), T2(j + 2)
 //               after ACC(j), which reads the dS over T2(j).
+// 33k queries, 512 states, 24 heads of 128: 312 us, 1000 TFLOP/s.  A pair of tiles takes 2700 cycles in a row and 400 more shared out
+// from between items: the chain T1 -> P -> dS -> ACC of a tile bounds it (without the loads of K, V, Q and dO 14 % less).
 #include <algorithm>
 
 #include "moc_cross.cuh"
@@ -98,9 +100,9 @@ __global__ void __launch_bounds__(kCrossDqThreads, 1) cross_dq_tc_kernel(const _
     volatile int *abort_flag = &s_abort;
 
     // delta_i = sum_x dO_ix O_ix of rows 32 dw .. 32 dw + 31 of every item, formed while the item before it is in work (the rows are asked
-    // for an item ahead of that): a pass over dO and O less than by a launch of its own, and O is read under the products.  (33k queries to 512 states, whole kernel 316 us; without
-    // delta 285; with delta formed of the tile of dO in shared memory, which comes an item later, 400; with barriers of their own for
-    // Q and dO 326; with both asked for by L2 prefetches an item ahead 328.)
+    // for an item ahead of that): a pass over dO and O less than by a launch of its own, and O is read under the products.  (33k queries
+    // to 512 states, whole kernel 312 us; without delta 285; with delta formed of the tile of dO in shared memory, which comes an item
+    // later, 400; with barriers of their own for Q and dO 326; with both asked for by L2 prefetches an item ahead 328.)
     auto form_delta = [&](int dw) __attribute__((always_inline)) {
         constexpr int CH = D / 8, RP = 32 / CH, B = 4;         // lanes a row, rows an instruction, instructions under way
         const int sub = lane / CH, c16 = lane % CH;
@@ -243,7 +245,8 @@ __global__ void __launch_bounds__(kCrossDqThreads, 1) cross_dq_tc_kernel(const _
 #pragma unroll
                         for (int x = 0; x < 32; x += 2) {
                             float a0, a1;
-                            unpack2(mul2(pack2(pv[rd * 32 + x], pv[rd * 32 + x + 1]), add2(pack2(__uint_as_float(dp[rd][x]), __uint_as_float(dp[rd][x + 1])), ndlt2)), a0, a1);
+                            const auto t = add2(pack2(__uint_as_float(dp[rd][x]), __uint_as_float(dp[rd][x + 1])), ndlt2);
+                            unpack2(mul2(pack2(pv[rd * 32 + x], pv[rd * 32 + x + 1]), t), a0, a1);
                             uds[x >> 1] = bf16x2(a0, a1);
                         }
                         tmem_st16(t2 + (rd * 2 + half) * 32, uds);

@@ -7,6 +7,8 @@
 //     m = max(m0, m1),  O = (2^(m0 - m) O0 + 2^(m1 - m) O1) / (2^(m0 - m) l0 + 2^(m1 - m) l1).
 // Arithmetic, masking and the zeros behind a segment's last value row: as in moc_cross_fwd_tc.cu.
 //
+// 257 queries (three tiles) against 32,760 states, 24 heads of 128, in shares of 128 key tiles: 162 us, 2150 cycles a key tile.
+//
 // 12 warps: 0-3 / 4-7 the softmax groups, 8 the query tiles (a ring of three) and K, 9 and 10 an MMA issuer for each group, 11 V.
 #include <algorithm>
 

@@ -11,6 +11,8 @@
 // A lane holds four pairs of channels of a row (16 lanes a row at d = 128, 8 at d = 64), the first channels of two pairs in one packed register and
 // the second ones in another, whichever channels the pairs are of: the norm, the rotation and their gradients are packed multiply-adds, and the
 // rotation needs no other lane.
+// 33k tokens, 24 + 24 heads of 128, bf16: forward 131 us, 6.2 TB/s (94 % of what a copy reaches); backward 219 us, 5.5 TB/s: there the
+// instructions of a row (some 110) keep the loads from being closer together.
 // Where there are too few tokens to fill the GPU, a token's heads are dealt to several warps.
 #include <algorithm>
 #include <math.h>
@@ -384,7 +386,7 @@ static int launch_norm_rope_t(const moc_rope *r, RopeParams &a, float *dw_q, flo
     for (int z = 0; z < 2; ++z) a.units[z] = (a.side[z].heads + rows - 1) / rows;
     const int units = a.units[0] + a.units[1];
     // A warp takes all of a token's heads, unless that leaves warps without work: then as many batches of rows as give every warp
-    // one (the angles are made once for each, some 200 instructions beside 350 a batch).
+    // one (each forms the angles of its token again).
     const int64_t warps = (int64_t)n_sm * per_sm * kRopeWarps;
     int split = (int)std::min<int64_t>(units, (warps + a.n_tokens - 1) / a.n_tokens);
     a.per_warp = (units + split - 1) / split;
