@@ -289,7 +289,9 @@ __global__ void __launch_bounds__(kRopeWarps * 32, RopeBatch<X, BWD>::BLOCKS) no
                     uint64_t r2 = 0;
                     if (norm) {
                         const uint64_t ss = fma2(v.b[1], v.b[1], fma2(v.b[0], v.b[0], fma2(v.a[1], v.a[1], mul2(v.a[0], v.a[0]))));
-                        r2 = both(rsqrtf(row_sum<LPR>(sum2(ss)) * p.inv_d + p.eps));
+                        const float mean = row_sum<LPR>(sum2(ss)) * p.inv_d + p.eps;
+                        // (of a row that is not there, and without an eps, 0 * inf would not be 0 in the sum for dw)
+                        r2 = both(!BWD || y * RPW < left ? rsqrtf(mean) : 0.f);
 #pragma unroll
                         for (int k = 0; k < 2; ++k) { v.a[k] = mul2(v.a[k], r2); v.b[k] = mul2(v.b[k], r2); }
                     }

@@ -138,6 +138,24 @@ def test_special_values_stay_in_their_rows():
     assert bad.nonzero().tolist() == [[1, 2], [2, 4]]
 
 
+@pytest.mark.parametrize("case", [(6, 5, 3, 128, (44, 42, 42), False, "bf16", True), (9, 5, 1, 64, (16, 24, 24), True, "fp32", True)])
+def test_no_eps_and_heads_that_leave_lanes_without_a_row(case):
+    L, hq, hk, d, ax, halves, dtype, norm = case
+    x, w, pos, dy, axis, freq = _make(*case, seed=7)
+    op = MocRope.from_axes(d, ax, eps=0.0, halves=halves)
+    xd, dyd = x.cuda().transpose(0, 1), dy.cuda()
+    dx = torch.empty(hq + hk, L, d, dtype=x.dtype, device="cuda")
+    dw = [torch.empty(d, device="cuda") for _ in range(2)]
+    op.moc_norm_rope_bwd(pos.cuda(), xd[:hq], w[0].cuda(), dyd[:hq], dx[:hq], dw[0], op.new_workspace(), xd[hq:], w[1].cuda(), dyd[hq:],
+                         dx[hq:], dw[1])
+    x64 = x.double().transpose(0, 1)
+    for z, heads in ((0, slice(0, hq)), (1, slice(hq, hq + hk))):
+        (want, tol), (want_w, tol_w) = R.norm_rope_bwd(x64[heads], w[z], pos, axis, freq, halves, 0.0, dy[heads].double(),
+                                                       R.U32 if dtype == "fp32" else R.U16)
+        R.check("dx", dx[heads], want, tol)
+        R.check("dw", dw[z], want_w, tol_w)
+
+
 def test_graph_other_stream_and_refusals_of_the_binding():
     L, h, d = 64, 4, 128
     gen = torch.Generator().manual_seed(6)
