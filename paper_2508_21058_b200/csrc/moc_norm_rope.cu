@@ -6,9 +6,10 @@
 //   dx = r (w g - xh mean_c(w g xh)).
 //
 // Both are bound by HBM where instructions do not get in the way: each value is read once and written once, and what a row needs
-// beside its own values is shared by all heads of a token.  So a warp takes a token and walks its heads: the angles - formed in turns, in 64
-// bits, reduced to a part of a turn and only then rounded to 32, so that far positions lose nothing - are made once for all of them.
-// A lane holds four pairs of channels of a row (16 lanes a row at d = 128, 8 at d = 64), the first channels of two pairs in one packed register and
+// beside its own values is shared by all heads of a token.  So a warp takes a token and walks its heads - or, of few heads, each of its lane
+// groups takes a token: the angles - formed in turns, in 64 bits, reduced to a part of a turn and only then rounded to 32, so that far
+// positions lose nothing - are made once for all of them.
+// A lane group is 16 lanes, at d = 64 eight.  A lane holds four pairs of channels of a row, the first channels of two pairs in one packed register and
 // the second ones in another, whichever channels the pairs are of: the norm, the rotation and their gradients are packed multiply-adds, and the
 // rotation needs no other lane.
 // 33k tokens, 24 + 24 heads of 128, bf16: forward 131 us, 6.2 TB/s (94 % of what a copy reaches); backward 219 us, 5.5 TB/s: there the
@@ -43,7 +44,7 @@ struct moc_rope {
 
 namespace moc {
 
-constexpr int kRopeWarps = 8;         // warps per block, each with a token of its own
+constexpr int kRopeWarps = 8;         // warps per block, each with tokens of its own
 
 // one of the two tensors of a call
 struct RopeSide {
@@ -60,8 +61,8 @@ struct RopeParams {
     const int32_t *pos;
     float *part;                      // backward: [blocks][2][d] sums for dw
     int n_tokens, n_axes, n_pairs;
-    int units[2];                     // batches of rows that a token's heads make
-    int per_warp, n_split;            // batches a warp takes, warps a token has
+    int units[2];                     // batches that a token's heads make
+    int per_warp, n_split;            // batches a warp takes, warps that share a token
     float eps, inv_d;
 };
 
@@ -219,8 +220,8 @@ struct RopeBatch {
     static constexpr int BLOCKS = BWD ? 2 : 3;
 };
 
-// FULL: every channel is turned
-template <int D, bool HALVES, bool FULL, typename X, bool BWD>
+// FULL: every channel is turned.  BY_TOKEN: the lane groups of a warp have a token each; otherwise heads of one token in turn.
+template <int D, bool HALVES, bool FULL, bool BY_TOKEN, typename X, bool BWD>
 __global__ void __launch_bounds__(kRopeWarps * 32, RopeBatch<X, BWD>::BLOCKS) norm_rope_kernel(const __grid_constant__ RopeTable tab, const RopeParams p) {
     using RB = RopeBatch<X, BWD>;
     using Y = typename std::conditional<BWD, X, __nv_bfloat16>::type;
@@ -244,11 +245,15 @@ __global__ void __launch_bounds__(kRopeWarps * 32, RopeBatch<X, BWD>::BLOCKS) no
     const int turned = p.n_pairs - chunk * 4 >= 4 ? 15 : p.n_pairs > chunk * 4 ? (1 << (p.n_pairs - chunk * 4)) - 1 : 0;
     Angles ang;
     Pairs acc[BWD ? 2 : 1] = {};
-    const int64_t n_items = (int64_t)p.n_tokens * p.n_split;
+    constexpr int N_TOK = BY_TOKEN ? RPW : 1, STEP = BY_TOKEN ? 1 : RPW;      // of a warp: tokens, and heads of a token at a time
+    const int64_t n_items = ((int64_t)p.n_tokens + N_TOK - 1) / N_TOK * p.n_split;
     for (int64_t item = (int64_t)blockIdx.x * kRopeWarps + warp; item < n_items; item += (int64_t)gridDim.x * kRopeWarps) {
-        // (a token is split only where there are few: 32 bits will do)
-        const unsigned tok = p.n_split == 1 ? (unsigned)item : (unsigned)item / (unsigned)p.n_split;
-        const int share = (int)((unsigned)item - tok * (unsigned)p.n_split);
+        // (tokens' heads are split only where there are few tokens: 32 bits will do)
+        const unsigned group = p.n_split == 1 ? (unsigned)item : (unsigned)item / (unsigned)p.n_split;
+        const int share = (int)((unsigned)item - group * (unsigned)p.n_split);
+        const int64_t mine = (int64_t)group * N_TOK + (BY_TOKEN ? sub : 0);
+        const bool there = !BY_TOKEN || mine < p.n_tokens;     // the last tokens may be fewer
+        const int64_t tok = there ? mine : p.n_tokens - 1;
         const int u_first = share * p.per_warp, u_end = min(p.units[0] + p.units[1], u_first + p.per_warp);
         bool made = false;
 #pragma unroll
@@ -257,41 +262,41 @@ __global__ void __launch_bounds__(kRopeWarps * 32, RopeBatch<X, BWD>::BLOCKS) no
             if (first >= last) continue;
             const RopeSide &sd = p.side[z];
             const bool norm = sd.w != nullptr;
-            int h = first * (U * RPW) + sub;                   // this lane's first head of the batch
-            const X *x = static_cast<const X *>(sd.x) + (int64_t)tok * sd.x_tok + (int64_t)h * sd.x_head;
-            const __nv_bfloat16 *dy = BWD ? sd.dy + (int64_t)tok * sd.dy_tok + (int64_t)h * sd.dy_head : nullptr;
-            Y *out = static_cast<Y *>(sd.out) + (int64_t)tok * sd.out_tok + (int64_t)h * sd.out_head;
+            int h = first * U * STEP + (BY_TOKEN ? 0 : sub); // this lane's first head of the batch
+            const X *x = static_cast<const X *>(sd.x) + tok * sd.x_tok + (int64_t)h * sd.x_head;
+            const __nv_bfloat16 *dy = BWD ? sd.dy + tok * sd.dy_tok + (int64_t)h * sd.dy_head : nullptr;
+            Y *out = static_cast<Y *>(sd.out) + tok * sd.out_tok + (int64_t)h * sd.out_head;
             const ulonglong2 wa = *reinterpret_cast<const ulonglong2 *>(&s_w[z][chunk * 8]), wb = *reinterpret_cast<const ulonglong2 *>(&s_w[z][chunk * 8 + 4]);
 #pragma unroll 1
-            for (int u = first; u < last; ++u, h += U * RPW) {
+            for (int u = first; u < last; ++u, h += U * STEP) {
                 Raw<X> rx[U];
                 Raw<__nv_bfloat16> rg[BWD ? U : 1];
-                const int left = sd.heads - h;
+                const int left = there ? sd.heads - h : 0, most = sd.heads - u * U * STEP;     // of this lane, of any
 #pragma unroll
                 for (int y = 0; y < U; ++y) {
                     rx[y] = {};
-                    if (y * RPW < left && (!BWD || norm)) rx[y].template load<HALVES>(x, ch);
-                    x += RPW * sd.x_head;
+                    if (y * STEP < left && (!BWD || norm)) rx[y].template load<HALVES>(x, ch);
+                    x += STEP * sd.x_head;
                     if constexpr (BWD) {
                         rg[y] = {};
-                        if (y * RPW < left) rg[y].template load<HALVES>(dy, ch);
-                        dy += RPW * sd.dy_head;
+                        if (y * STEP < left) rg[y].template load<HALVES>(dy, ch);
+                        dy += STEP * sd.dy_head;
                     }
                 }
                 if (!made) {                                   // while the first rows are on their way
-                    ang.make(s_turns, s_axis, p.pos + (int64_t)tok * p.n_axes, chunk, p.n_pairs);
+                    ang.make(s_turns, s_axis, p.pos + tok * p.n_axes, chunk, p.n_pairs);
                     made = true;
                 }
 #pragma unroll
                 for (int y = 0; y < U; ++y) {
-                    if (y > 0 && y * RPW >= left + sub) break;      // (no lane has such a row)
+                    if (y > 0 && y * STEP >= most) break;           // (no lane has such a row)
                     Pairs v = rx[y].template get<HALVES>();
                     uint64_t r2 = 0;
                     if (norm) {
                         const uint64_t ss = fma2(v.b[1], v.b[1], fma2(v.b[0], v.b[0], fma2(v.a[1], v.a[1], mul2(v.a[0], v.a[0]))));
                         const float mean = row_sum<LPR>(sum2(ss)) * p.inv_d + p.eps;
                         // (of a row that is not there, and without an eps, 0 * inf would not be 0 in the sum for dw)
-                        r2 = both(!BWD || y * RPW < left ? rsqrtf(mean) : 0.f);
+                        r2 = both(!BWD || y * STEP < left ? rsqrtf(mean) : 0.f);
 #pragma unroll
                         for (int k = 0; k < 2; ++k) { v.a[k] = mul2(v.a[k], r2); v.b[k] = mul2(v.b[k], r2); }
                     }
@@ -301,7 +306,7 @@ __global__ void __launch_bounds__(kRopeWarps * 32, RopeBatch<X, BWD>::BLOCKS) no
                             v.b[0] = mul2(v.b[0], wb.x); v.b[1] = mul2(v.b[1], wb.y);
                         }
                         const Pairs t = ang.template turn<false, FULL>(v, turned);
-                        if (y * RPW < left) put_pairs<HALVES>(out, ch, t);
+                        if (y * STEP < left) put_pairs<HALVES>(out, ch, t);
                     } else {
                         Pairs g = ang.template turn<true, FULL>(rg[y].template get<HALVES>(), turned);
                         if (norm) {
@@ -320,9 +325,9 @@ __global__ void __launch_bounds__(kRopeWarps * 32, RopeBatch<X, BWD>::BLOCKS) no
                                 g.b[k] = mul2(fma2(v.b[k], nm, g.b[k]), r2);
                             }
                         }
-                        if (y * RPW < left) put_pairs<HALVES>(out, ch, g);
+                        if (y * STEP < left) put_pairs<HALVES>(out, ch, g);
                     }
-                    out += RPW * sd.out_head;
+                    out += STEP * sd.out_head;
                 }
             }
         }
@@ -381,27 +386,44 @@ __global__ void __launch_bounds__(1024) norm_rope_dw_kernel(const float *part, i
 // the most blocks that a backward launch has: what the workspace holds sums of
 constexpr int kRopeMaxBlocks = 2048;
 
-template <int D, bool HALVES, bool FULL, typename X, bool BWD>
-static int launch_norm_rope_t(const moc_rope *r, RopeParams &a, float *dw_q, float *dw_k, int n_sm, cudaStream_t s) {
+template <int D, bool HALVES, bool FULL, bool BY_TOKEN, typename X, bool BWD>
+static int launch_norm_rope_u(const moc_rope *r, RopeParams &a, float *dw_q, float *dw_k, int n_sm, cudaStream_t s) {
     using RB = RopeBatch<X, BWD>;
-    constexpr int rows = RB::U * 32 / (D / 8), per_sm = RB::BLOCKS;      // rows of a batch
-    for (int z = 0; z < 2; ++z) a.units[z] = (a.side[z].heads + rows - 1) / rows;
+    constexpr int RPW = 32 / (D / 8), batch = RB::U * (BY_TOKEN ? 1 : RPW), per_sm = RB::BLOCKS;      // heads of a batch
+    for (int z = 0; z < 2; ++z) a.units[z] = (a.side[z].heads + batch - 1) / batch;
     const int units = a.units[0] + a.units[1];
-    // A warp takes all of a token's heads, unless that leaves warps without work: then as many batches of rows as give every warp
-    // one (each forms the angles of its token again).
-    const int64_t warps = (int64_t)n_sm * per_sm * kRopeWarps;
-    int split = (int)std::min<int64_t>(units, (warps + a.n_tokens - 1) / a.n_tokens);
+    // A warp takes all of its tokens' heads, unless that leaves warps without work: then as many batches of heads as give every warp
+    // one (each forms the angles of its tokens again).
+    const int64_t warps = (int64_t)n_sm * per_sm * kRopeWarps, groups = BY_TOKEN ? ((int64_t)a.n_tokens + RPW - 1) / RPW : a.n_tokens;
+    int split = (int)std::min<int64_t>(units, (warps + groups - 1) / groups);
     a.per_warp = (units + split - 1) / split;
     a.n_split = (units + a.per_warp - 1) / a.per_warp;
-    const int64_t items = (int64_t)a.n_tokens * a.n_split;
+    const int64_t items = groups * a.n_split;
     const unsigned grid = (unsigned)std::min<int64_t>({(items + kRopeWarps - 1) / kRopeWarps, (int64_t)n_sm * per_sm, (int64_t)kRopeMaxBlocks});
-    norm_rope_kernel<D, HALVES, FULL, X, BWD><<<grid, kRopeWarps * 32, 0, s>>>(r->tab, a);
+    norm_rope_kernel<D, HALVES, FULL, BY_TOKEN, X, BWD><<<grid, kRopeWarps * 32, 0, s>>>(r->tab, a);
     MOC_LAUNCH_CHECK();
     if (BWD && (dw_q || dw_k)) {
         MOC_CUDA_TRY(launch_early(true, norm_rope_dw_kernel, 2 * D / 32, 1024, 0, s, (const float *)a.part, (int)grid, D, dw_q, dw_k));
         MOC_LAUNCH_CHECK();
     }
     return MOC_OK;
+}
+
+// The lane groups of a warp have heads of one token in turn, next to one another in a projection; or, where that leaves more lanes without a
+// row, a token each.  (33k tokens, bf16, forward and backward, heads of one token and a token each: 12 + 12 heads of 128 70 / 122 and
+// 73 / 120 us; 66k tokens, 6 + 2 heads of 64, 71 / 118 and 34 / 54; 264k tokens, 1 + 1 head of 128, 248 / 396 and 132 / 210.  An fp32
+// projection, 6.4k tokens, 24 + 24 heads of 128, 40 / 70 and 43 / 80.  With the step from head to head as an argument of one kernel
+// instead, the same cases were 77 / 138, 37 / 57 and 153 / 255.)
+template <int D, bool HALVES, bool FULL, typename X, bool BWD>
+static int launch_norm_rope_t(const moc_rope *r, RopeParams &a, float *dw_q, float *dw_k, int n_sm, cudaStream_t s) {
+    constexpr int U = RopeBatch<X, BWD>::U, RPW = 32 / (D / 8);
+    int in_turn = 0, a_token = 0;                               // rows that a lane group has room for, at a token
+    for (const RopeSide &sd : a.side) {
+        in_turn += (sd.heads + U * RPW - 1) / (U * RPW) * RPW;
+        a_token += (sd.heads + U - 1) / U;
+    }
+    return a_token < in_turn ? launch_norm_rope_u<D, HALVES, FULL, true, X, BWD>(r, a, dw_q, dw_k, n_sm, s)
+                             : launch_norm_rope_u<D, HALVES, FULL, false, X, BWD>(r, a, dw_q, dw_k, n_sm, s);
 }
 
 template <bool BWD>

@@ -138,7 +138,8 @@ def test_special_values_stay_in_their_rows():
     assert bad.nonzero().tolist() == [[1, 2], [2, 4]]
 
 
-@pytest.mark.parametrize("case", [(6, 5, 3, 128, (44, 42, 42), False, "bf16", True), (9, 5, 1, 64, (16, 24, 24), True, "fp32", True)])
+@pytest.mark.parametrize("case", [(6, 5, 3, 128, (44, 42, 42), False, "bf16", True), (9, 5, 1, 64, (16, 24, 24), True, "fp32", True),
+                                  (7, 11, 12, 128, (44, 42, 42), False, "bf16", True), (1, 23, 7, 64, (64,), True, "bf16", True)])
 def test_no_eps_and_heads_that_leave_lanes_without_a_row(case):
     L, hq, hk, d, ax, halves, dtype, norm = case
     x, w, pos, dy, axis, freq = _make(*case, seed=7)
