@@ -343,6 +343,7 @@ template <int D>
 __global__ void __launch_bounds__(256) cross_sum_dq_kernel(const CrossMerge *merges, const float *part, int prows, CrossRows dQ) {
     const CrossMerge m = merges[blockIdx.x];
     const int h = blockIdx.y, at = (blockIdx.z * 256 + threadIdx.x) * 4, row = at / D, col = at % D;
+    next_may_start();
     previous_done();
     if (row < m.rows)
         sum_row<D>(part + ((size_t)h * prows + m.slot + row) * D + col, (size_t)m.rows * D, m.n, dQ.row(h, m.q0 + row) + col);
@@ -413,6 +414,14 @@ extern "C" int moc_cross_create(const moc_cross_problem *pr, moc_cross **out) {
             if (c->d_blob) cudaFree(c->d_blob);
             delete c;
             return MOC_ERR_CUDA;
+        }
+        int r = MOC_OK;
+        for (auto prepare : {prepare_cross_fwd, prepare_cross_solo, prepare_cross_few, prepare_cross_dq, prepare_cross_dkv})
+            if (!r) r = prepare(c);
+        if (r) {
+            cudaFree(c->d_blob);
+            delete c;
+            return r;
         }
         char *d = static_cast<char *>(c->d_blob);
         c->d_items = (CrossItem *)(d + a); c->d_dq_items = (CrossItem *)(d + b); c->d_few = (CrossFew *)(d + fe); c->d_solo = (CrossItem *)(d + so);
@@ -485,6 +494,7 @@ extern "C" int moc_cross_attend_bwd(const moc_cross *c, const moc_rows *Q, const
     cudaStream_t s = (cudaStream_t)stream;
     if (c->Lq > 0) {
         if (int r = launch_cross_dq(c, Q, K, V, O, lse, dO, dQ, ws, s)) return r;
+        // (each of the launches that follow waits for the one before it)
         if (!c->dq_merges.empty()) {
             const dim3 g2((unsigned)c->dq_merges.size(), c->H, c->d / 8);      // 1024 values a block
             const float *part = ws_ptr<float>(ws, c->ws.part_dq);

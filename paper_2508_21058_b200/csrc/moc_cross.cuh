@@ -56,6 +56,7 @@ struct moc_cross {
     int32_t *d_piece_off;
     moc::CrossSum *d_sums;
     moc::CrossLayout ws;
+    size_t dq_smem = 0, dkv_smem = 0;                  // shared memory of their launches
 };
 
 namespace moc {
@@ -84,6 +85,13 @@ __device__ __forceinline__ int cross_items(int n_all) {
 // asks for an item's description ahead of its use
 __device__ __forceinline__ void prefetch_item(const CrossItem *item) { asm volatile("prefetch.global.L1 [%0];" ::"l"(item)); }
 #endif
+
+// what the kernels of a plan's launches need of the runtime, once
+int prepare_cross_fwd(moc_cross *c);
+int prepare_cross_solo(moc_cross *c);
+int prepare_cross_few(moc_cross *c);
+int prepare_cross_dq(moc_cross *c);
+int prepare_cross_dkv(moc_cross *c);
 
 int launch_cross_solo(const moc_cross *c, const moc_rows *Q, const moc_rows *K, const moc_rows *V, const moc_rows *O, float *lse, void *ws, bool first, cudaStream_t s);
 int launch_cross_few(const moc_cross *c, const moc_rows *Q, const moc_rows *K, const moc_rows *V, const moc_rows *O, float *lse, void *ws,

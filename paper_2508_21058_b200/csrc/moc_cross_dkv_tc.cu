@@ -65,6 +65,7 @@ __global__ void __launch_bounds__(kCrossKvThreads, 1) cross_dkv_tc_kernel(const 
     asm volatile("mov.u32 %0, %%dynamic_smem_size;" : "=r"(dyn_bytes));
     if ((sbase - smem_u32(smem_raw)) + (uint32_t)(2 + kCrossY1 + kCrossY2) * TILE_BYTES > dyn_bytes) {
         // the launch gave less shared memory than the tiles need: report, touch nothing
+        previous_done();
         if (threadIdx.x == 0) report_abort(p.status, CB_SMEM);
         return;
     }
@@ -87,6 +88,7 @@ __global__ void __launch_bounds__(kCrossKvThreads, 1) cross_dkv_tc_kernel(const 
     // TMEM columns: T1 [0,128)  T2 [128,256)  ACC1 [256,384)  ACC2 [384,512)
     const uint32_t tmem = tmem_slot;
     volatile int *abort_flag = &s_abort;
+    previous_done();
     const int piece0 = p.piece_off[blockIdx.x], piece1 = p.piece_off[blockIdx.x + 1];
 
     if (warp < 8) {
@@ -450,6 +452,20 @@ __global__ void __launch_bounds__(kCrossKvThreads, 1) cross_dkv_tc_kernel(const 
     if (threadIdx.x == 0) report_abort(p.status, s_abort);
 }
 
+int prepare_cross_dkv(moc_cross *c) {
+    const void *kernel = c->d == 128 ? (const void *)cross_dkv_tc_kernel<128> : (const void *)cross_dkv_tc_kernel<64>;
+    // seven tiles, always the d = 128 footprint, so that CTAs, which each take all of the tensor memory, never share an SM
+    const size_t tiles = (size_t)(2 + kCrossY1 + kCrossY2) * 128 * 128 * 2;
+    int optin = 0;
+    cudaFuncAttributes fa;
+    MOC_CUDA_TRY(cudaDeviceGetAttribute(&optin, cudaDevAttrMaxSharedMemoryPerBlockOptin, c->device));
+    MOC_CUDA_TRY(cudaFuncGetAttributes(&fa, kernel));
+    c->dkv_smem = std::min(tiles + 1024, (size_t)optin - fa.sharedSizeBytes);
+    if (c->dkv_smem < tiles) return MOC_ERR_SHAPE;
+    MOC_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)c->dkv_smem));
+    return MOC_OK;
+}
+
 template <int D>
 static int cross_dkv_d(const moc_cross *c, const moc_rows *Q, const moc_rows *K, const moc_rows *V, const float *lse, const moc_rows *dO,
                        const moc_rows *dK, const moc_rows *dV, void *ws, cudaStream_t s) {
@@ -466,16 +482,11 @@ static int cross_dkv_d(const moc_cross *c, const moc_rows *Q, const moc_rows *K,
     a.status = ws_ptr<int>(ws, c->ws.status);
     a.scale = c->scale; a.scale_log2 = c->scale * 1.4426950408889634f;
     a.wait = WaitBound::of(0);
-    // seven tiles, always the d = 128 footprint, so that CTAs, which each take all of the tensor memory, never share an SM
-    const size_t tiles = (size_t)(2 + kCrossY1 + kCrossY2) * 128 * 128 * 2;
-    int optin = 0;
-    cudaFuncAttributes fa;
-    MOC_CUDA_TRY(cudaDeviceGetAttribute(&optin, cudaDevAttrMaxSharedMemoryPerBlockOptin, c->device));
-    MOC_CUDA_TRY(cudaFuncGetAttributes(&fa, cross_dkv_tc_kernel<D>));
-    const size_t smem = std::min(tiles + 1024, (size_t)optin - fa.sharedSizeBytes);
-    if (smem < tiles) return MOC_ERR_SHAPE;
-    MOC_CUDA_TRY(cudaFuncSetAttribute(cross_dkv_tc_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-    cross_dkv_tc_kernel<D><<<(unsigned)(c->piece_off.size() - 1), kCrossKvThreads, smem, s>>>(tmK, tmV, tmQ, tmdO, a);
+    // A short launch begins while dQ's, or the one that adds up its shares, ends: of these it needs delta (82 queries, 755 states, 6 heads, both
+    // directions in a graph: 34.2 us, 35.1 one after the other).  A long one does not: its CTAs would lie where SMs come free, not with
+    // neighbours that stream the same queries side by side (33k queries, 512 states, 24 heads: 845 us, 836 one after the other).
+    const bool early = c->pieces.size() <= (size_t)c->n_sm;
+    MOC_CUDA_TRY(launch_early(early, cross_dkv_tc_kernel<D>, (unsigned)(c->piece_off.size() - 1), kCrossKvThreads, c->dkv_smem, s, tmK, tmV, tmQ, tmdO, a));
     MOC_LAUNCH_CHECK();
     return MOC_OK;
 }

@@ -476,6 +476,20 @@ __global__ void __launch_bounds__(kCrossDqThreads, 1) cross_dq_tc_kernel(const _
     if (threadIdx.x == 0) report_abort(p.status, s_abort);
 }
 
+int prepare_cross_dq(moc_cross *c) {
+    const void *kernel = c->d == 128 ? (const void *)cross_dq_tc_kernel<128> : (const void *)cross_dq_tc_kernel<64>;
+    // seven tiles, always the d = 128 footprint, so that CTAs, which each take all of the tensor memory, never share an SM
+    const size_t tiles = (size_t)(2 + kCrossKStages + kCrossVStages) * 128 * 128 * 2;
+    int optin = 0;
+    cudaFuncAttributes fa;
+    MOC_CUDA_TRY(cudaDeviceGetAttribute(&optin, cudaDevAttrMaxSharedMemoryPerBlockOptin, c->device));
+    MOC_CUDA_TRY(cudaFuncGetAttributes(&fa, kernel));
+    c->dq_smem = std::min(tiles + 1024, (size_t)optin - fa.sharedSizeBytes);
+    if (c->dq_smem < tiles) return MOC_ERR_SHAPE;
+    MOC_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)c->dq_smem));
+    return MOC_OK;
+}
+
 template <int D>
 static int cross_dq_d(const moc_cross *c, const moc_rows *Q, const moc_rows *K, const moc_rows *V, const moc_rows *O, const float *lse, const moc_rows *dO,
                       const moc_rows *dQ, void *ws, cudaStream_t s) {
@@ -497,16 +511,7 @@ static int cross_dq_d(const moc_cross *c, const moc_rows *Q, const moc_rows *K, 
     a.status = ws_ptr<int>(ws, c->ws.status);
     a.scale = c->scale; a.scale_log2 = c->scale * 1.4426950408889634f;
     a.wait = WaitBound::of(0);
-    // seven tiles, always the d = 128 footprint, so that CTAs, which each take all of the tensor memory, never share an SM
-    const size_t tiles = (size_t)(2 + kCrossKStages + kCrossVStages) * 128 * 128 * 2;
-    int optin = 0;
-    cudaFuncAttributes fa;
-    MOC_CUDA_TRY(cudaDeviceGetAttribute(&optin, cudaDevAttrMaxSharedMemoryPerBlockOptin, c->device));
-    MOC_CUDA_TRY(cudaFuncGetAttributes(&fa, cross_dq_tc_kernel<D>));
-    const size_t smem = std::min(tiles + 1024, (size_t)optin - fa.sharedSizeBytes);
-    if (smem < tiles) return MOC_ERR_SHAPE;
-    MOC_CUDA_TRY(cudaFuncSetAttribute(cross_dq_tc_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-    cross_dq_tc_kernel<D><<<cross_grid(c, c->dq_items.size()), kCrossDqThreads, smem, s>>>(tmQ, tmdO, tmK, tmV, tmK16, tmV16, a);
+    cross_dq_tc_kernel<D><<<cross_grid(c, c->dq_items.size()), kCrossDqThreads, c->dq_smem, s>>>(tmQ, tmdO, tmK, tmV, tmK16, tmV16, a);
     MOC_LAUNCH_CHECK();
     return MOC_OK;
 }

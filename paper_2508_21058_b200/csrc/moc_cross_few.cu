@@ -201,11 +201,21 @@ __global__ void __launch_bounds__(kFewThreads, 3) cross_few_kernel(const CrossFe
     }
 }
 
+static constexpr size_t few_smem(int d) { return (size_t)kFewStages * 2 * kFewKeys * d * 2; }
+
+int prepare_cross_few(moc_cross *c) {
+    const int r = std::min(std::max(c->few_rows, 1), 4) - 1;
+    const void *const k64[4] = {(const void *)cross_few_kernel<64, 1>, (const void *)cross_few_kernel<64, 2>, (const void *)cross_few_kernel<64, 3>,
+                                (const void *)cross_few_kernel<64, 4>},
+               *const k128[4] = {(const void *)cross_few_kernel<128, 1>, (const void *)cross_few_kernel<128, 2>, (const void *)cross_few_kernel<128, 3>,
+                                 (const void *)cross_few_kernel<128, 4>};
+    MOC_CUDA_TRY(cudaFuncSetAttribute(c->d == 128 ? k128[r] : k64[r], cudaFuncAttributeMaxDynamicSharedMemorySize, (int)few_smem(c->d)));
+    return MOC_OK;
+}
+
 template <int D, int R>
 static int cross_few_t(const moc_cross *c, const CrossFewParams &a, cudaStream_t s) {
-    constexpr size_t smem = (size_t)kFewStages * 2 * kFewKeys * D * 2;
-    MOC_CUDA_TRY(cudaFuncSetAttribute(cross_few_kernel<D, R>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-    cross_few_kernel<D, R><<<(unsigned)(c->few.size() * c->Hkv), kFewThreads, smem, s>>>(a);
+    cross_few_kernel<D, R><<<(unsigned)(c->few.size() * c->Hkv), kFewThreads, few_smem(D), s>>>(a);
     MOC_LAUNCH_CHECK();
     return MOC_OK;
 }

@@ -425,6 +425,15 @@ __global__ void __launch_bounds__(kCrossSoloThreads, 1) cross_solo_tc_kernel(con
     if (threadIdx.x == 0) report_abort(p.status, s_abort);
 }
 
+// always the d = 128 footprint: more than half an SM's shared memory, so that CTAs, which each take all of the tensor memory, never share one
+constexpr size_t kSmem = 7 * (size_t)128 * 128 * 2 + 1024;
+
+int prepare_cross_solo(moc_cross *c) {
+    const void *kernel = c->d == 128 ? (const void *)cross_solo_tc_kernel<128> : (const void *)cross_solo_tc_kernel<64>;
+    MOC_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem));
+    return MOC_OK;
+}
+
 template <int D>
 static int cross_solo_d(const moc_cross *c, const moc_rows *Q, const moc_rows *K, const moc_rows *V, const moc_rows *O, float *lse, void *ws,
                         bool first, cudaStream_t s) {
@@ -442,10 +451,7 @@ static int cross_solo_d(const moc_cross *c, const moc_rows *Q, const moc_rows *K
     a.status = ws_ptr<int>(ws, c->ws.status); a.first = first;
     a.scale_log2 = c->scale * 1.4426950408889634f;
     a.wait = WaitBound::of(0);
-    // always the d = 128 footprint: more than half an SM's shared memory, so that CTAs, which each take all of the tensor memory, never share one
-    const size_t smem = 7 * (size_t)128 * 128 * 2 + 1024;
-    MOC_CUDA_TRY(cudaFuncSetAttribute(cross_solo_tc_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-    cross_solo_tc_kernel<D><<<cross_grid(c, c->solo.size()), kCrossSoloThreads, smem, s>>>(tmQ, tmK, tmV, tmK16, tmV16, a);
+    cross_solo_tc_kernel<D><<<cross_grid(c, c->solo.size()), kCrossSoloThreads, kSmem, s>>>(tmQ, tmK, tmV, tmK16, tmV16, a);
     MOC_LAUNCH_CHECK();
     return MOC_OK;
 }
