@@ -310,9 +310,10 @@ int moc_cross_workspace_bytes(const moc_cross *cross, int with_bwd, size_t *byte
 
 /* O = softmax(scale Q K^T) V over the segment's states, lse (fp32, [n_heads][q_off[n_segments]] contiguous) = ln of the sum of
  * exp(scale q.k).  Q, O: bf16 rows of n_heads heads and q_off[n_segments] tokens (at least: rows behind them are neither read nor written);
- * K, V: of n_kv_heads heads and k_off[n_segments] tokens.  A query without states gets O = 0 and lse = -inf.  Padding is
- * not looked at: it may hold anything.  Products in bf16, fp32 accumulation and softmax (segments of up to eight rows of
- * the query heads that share a key head: fp32 throughout).  No tensor may overlap one that is written. */
+ * K, V: of n_kv_heads heads and k_off[n_segments] tokens.  A query without states gets O = 0 and lse = -inf.  A state whose score is
+ * -inf weighs nothing; a query that sees nothing else gets NaN and lse = -inf, as the formula gives.  Padding is not looked at: it
+ * may hold anything.  Products in bf16, fp32 accumulation and softmax (segments of up to eight rows of the query heads that share a
+ * key head: fp32 throughout).  No tensor may overlap one that is written. */
 int moc_cross_attend(const moc_cross *cross, const moc_rows *Q, const moc_rows *K, const moc_rows *V, const moc_rows *O, float *lse,
                      void *ws, void *stream);
 

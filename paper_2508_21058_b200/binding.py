@@ -94,6 +94,7 @@ def load_library():
     lib.moc_cross_attend.argtypes = [vp] + [rows] * 4 + [vp] * 3
     lib.moc_cross_attend_bwd.argtypes = [vp] + [rows] * 4 + [vp] + [rows] * 4 + [vp] * 2
     lib.moc_cross_get_status.argtypes = [vp, vp, vp, C.POINTER(i32), C.POINTER(i32)]
+    lib.moc_debug_cross_plan.argtypes = [C.POINTER(_CrossProblem), i32, C.POINTER(C.c_int64)]
     lib.moc_selected_pairs.argtypes = [vp, vp, vp, C.POINTER(C.c_int64)]
     lib.moc_get_status.argtypes = [vp, vp, vp, C.POINTER(i32), C.POINTER(i32)]
     lib.moc_launch_count.restype = C.c_int64
@@ -396,6 +397,26 @@ class MocRope:
             _check(code)
 
 
+def _cross_problem(n_heads, n_kv_heads, head_dim, q_off, k_off, k_len, softmax_scale):
+    """The C problem statement, and the host arrays it points to."""
+    qo, ko = np.ascontiguousarray(q_off, np.int32), np.ascontiguousarray(k_off, np.int32)
+    kl = None if k_len is None else np.ascontiguousarray(k_len, np.int32)
+    if qo.ndim != 1 or len(qo) < 1 or ko.shape != qo.shape or (kl is not None and kl.shape != (len(qo) - 1,)):
+        raise MocError(-3, "moc error -3: segment tables have inconsistent lengths")
+    pr = _CrossProblem(int(n_heads), int(n_kv_heads), int(head_dim), len(qo) - 1, float(softmax_scale), qo.ctypes.data, ko.ctypes.data,
+                       None if kl is None else kl.ctypes.data)
+    return pr, (qo, ko, kl)
+
+
+def debug_cross_plan(n_heads, n_kv_heads, head_dim, q_off, k_off, k_len=None, n_sm=148):
+    """Test hook, host only: what MocCross of the same arguments launches on n_sm SMs: items of the forward's three kernels, rows of
+    partial results, items of dQ, pieces of dK/dV and slots of their sums."""
+    pr, tables = _cross_problem(n_heads, n_kv_heads, head_dim, q_off, k_off, k_len, 0.0)
+    out = (C.c_int64 * 7)()
+    _check(load_library().moc_debug_cross_plan(C.byref(pr), int(n_sm), out))
+    return dict(zip(("two_tile", "one_tile", "few", "part_rows", "dq", "pieces", "slots"), out))
+
+
 class MocCross:
     """Owns a ``moc_cross``: attention of a stream's segments (shots, or sequences of a batch) to encoder states of another
     length.  q_off, k_off: [segments + 1] where each segment's queries and states begin; k_len: how many of them it has
@@ -404,12 +425,7 @@ class MocCross:
     def __init__(self, n_heads, n_kv_heads, head_dim, q_off, k_off, k_len=None, softmax_scale=0.0):
         self._lib = load_library()
         self._h = C.c_void_p(0)
-        qo, ko = np.ascontiguousarray(q_off, np.int32), np.ascontiguousarray(k_off, np.int32)
-        kl = None if k_len is None else np.ascontiguousarray(k_len, np.int32)
-        if qo.ndim != 1 or len(qo) < 1 or ko.shape != qo.shape or (kl is not None and kl.shape != (len(qo) - 1,)):
-            raise MocError(-3, "moc error -3: segment tables have inconsistent lengths")
-        pr = _CrossProblem(int(n_heads), int(n_kv_heads), int(head_dim), len(qo) - 1, float(softmax_scale), qo.ctypes.data, ko.ctypes.data,
-                           None if kl is None else kl.ctypes.data)
+        pr, (qo, ko, _) = _cross_problem(n_heads, n_kv_heads, head_dim, q_off, k_off, k_len, softmax_scale)
         _check(self._lib.moc_cross_create(C.byref(pr), C.byref(self._h)))
         self.H, self.Hkv, self.d = int(n_heads), int(n_kv_heads), int(head_dim)
         self.n_queries, self.n_states = int(qo[-1]), int(ko[-1])

@@ -276,7 +276,7 @@ __global__ void __launch_bounds__(256) cross_merge_kernel(const CrossMerge *merg
     previous_done();
     if (row >= m.rows) return;                                 // (WIDE: the whole block)
     const size_t at = (size_t)h * prows + m.slot + row;
-    float big = -INFINITY;
+    float big = kLowest;
     for (int i = lane; i < m.n; i += 32) big = fmaxf(big, part_lse[at + (size_t)i * m.rows]);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, o));
@@ -514,6 +514,25 @@ extern "C" int moc_cross_attend_bwd(const moc_cross *c, const moc_rows *Q, const
                                   CrossRows(dV)));
         MOC_LAUNCH_CHECK();
     }
+    return MOC_OK;
+}
+
+// Test hook, host only: the launches of a problem on a GPU of n_sm SMs.  out: items of the forward's kernels (two query tiles, one, few
+// queries) that have keys, and rows to put together; items of dQ that have keys; pieces of dK/dV; slots of their sums
+extern "C" int moc_debug_cross_plan(const moc_cross_problem *pr, int n_sm, int64_t *out) {
+    if (!pr || !out) return MOC_ERR_NULL;
+    if (int r = check_cross(pr)) return r;
+    if (n_sm < 1) return MOC_ERR_SHAPE;
+    moc_cross c = {};
+    c.n_sm = n_sm;
+    try {
+        derive_cross(&c, pr);
+    } catch (...) {
+        return MOC_ERR_CUDA;
+    }
+    auto with_keys = [](const std::vector<CrossItem> &items) { return std::count_if(items.begin(), items.end(), [](const CrossItem &i) { return i.n_keys > 0; }); };
+    out[0] = with_keys(c.items) * c.H; out[1] = (int64_t)c.solo.size() * c.H; out[2] = (int64_t)c.few.size() * c.Hkv; out[3] = (int64_t)c.prows * c.H;
+    out[4] = with_keys(c.dq_items) * c.H; out[5] = (int64_t)c.pieces.size(); out[6] = c.kv_slots;
     return MOC_OK;
 }
 

@@ -21,6 +21,11 @@ struct __align__(16) CrossPiece { int32_t h, k0, keys, q0, q1, u0, u1, slot; };
 struct __align__(16) CrossSum { int32_t h, k0, rows, slot, n, pad[3]; };
 
 constexpr int kCrossRows = 256;
+// Where a running maximum begins: below every score but not minus infinity, so that a score of minus infinity weighs 2^-inf = 0, not
+// 2^(inf - inf), also where a row has seen no other yet.  A row, or a share of its states, that sees no other has a sum of 0 and a log-sum-exp
+// of minus infinity.
+constexpr float kLowest = -3.402823466e38f;
+
 constexpr int kFewRows = 8;        // rows of a key head up to which a segment counts as one with few queries
 
 struct CrossLayout {

@@ -72,7 +72,7 @@ __global__ void __launch_bounds__(kFewThreads, 3) cross_few_kernel(const CrossFe
     const uint64_t c2 = pack2(p.scale_log2, p.scale_log2);
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        m[r] = -INFINITY;
+        m[r] = kLowest;
         l[r] = 0.f;
         const int at = it.r0 + min(r, it.nr - 1), h = hk * p.g + at / it.q_len, t = it.q0 + at % it.q_len;
 #pragma unroll
@@ -127,7 +127,7 @@ __global__ void __launch_bounds__(kFewThreads, 3) cross_few_kernel(const CrossFe
 #pragma unroll
                 for (int r = 0; r < R; ++r) {
                     if (there && sc[r] > m[r] + 8.f) {
-                        const float w = ex2(m[r] - sc[r]);     // (nothing yet: 2^-inf = 0)
+                        const float w = ex2(m[r] - sc[r]);     // (nothing yet: 0)
                         m[r] = sc[r];
                         l[r] *= w;
                         const uint64_t w2 = pack2(w, w);
@@ -159,7 +159,7 @@ __global__ void __launch_bounds__(kFewThreads, 3) cross_few_kernel(const CrossFe
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         const float big = fmaxf(fmaxf(m[r], __shfl_xor_sync(0xffffffffu, m[r], 8)), fmaxf(__shfl_xor_sync(0xffffffffu, m[r], 16), __shfl_xor_sync(0xffffffffu, m[r], 24)));
-        const float w = l[r] == 0.f ? 0.f : ex2(m[r] - big);   // (a group without a state has no maximum)
+        const float w = l[r] == 0.f ? 0.f : ex2(m[r] - big);   // (a group without a state, or without one that weighs)
         float sum = l[r] * w;
         sum += __shfl_xor_sync(0xffffffffu, sum, 8);
         sum += __shfl_xor_sync(0xffffffffu, sum, 16);
@@ -188,7 +188,8 @@ __global__ void __launch_bounds__(kFewThreads, 3) cross_few_kernel(const CrossFe
             a += w * s_o[y][r][c];
             b += w * s_o[y][r][c + 1];
         }
-        const float inv = 1.f / sum, lse = (big + log2f(sum)) * 0.6931471805599453f;
+        // (a share whose states all weigh nothing: its row is a sum of zeros, which has no weight in the sum of shares)
+        const float inv = it.slot >= 0 && sum == 0.f ? 1.f : 1.f / sum, lse = (big + log2f(sum)) * 0.6931471805599453f;
         const int at = it.r0 + r, h = hk * p.g + at / it.q_len, t = at % it.q_len;
         if (it.slot < 0) {
             *reinterpret_cast<uint32_t *>(p.O.row(h, it.q0 + t) + c) = bf16x2(a * inv, b * inv);

@@ -127,7 +127,7 @@ __global__ void __launch_bounds__(kCrossThreads, 1) cross_fwd_tc_kernel(const __
                 if (r < tile_rows) p.lse[(size_t)h * p.Lq + it.q0 + g * 128 + r] = -INFINITY;
                 continue;
             }
-            float m_run = -INFINITY, l_run = 0.f;
+            float m_run = kLowest, l_run = 0.f;
             for (int k = 0; k < it.n_keys; k += 128) {
                 const int valid = min(128, it.n_keys - k);
                 ok = mbar_wait(bar(S_FULL + g), bits & S_ODD, abort_flag, p.wait, CW_SFULL);
@@ -222,7 +222,8 @@ __global__ void __launch_bounds__(kCrossThreads, 1) cross_fwd_tc_kernel(const __
             // ---- results, in the 16 x 256-bit shape of the tensor memory: four lanes write 128 contiguous bytes of a row
             constexpr int CB = D / 64;
             const int l4 = lane >> 2, l2 = lane & 3, row = (warp & 3) * 32 + lane;
-            const float inv_l = 1.f / l_run, lse = (m_run + log2f(l_run)) * 0.6931471805599453f;
+            // (a share whose states all weigh nothing: its row is a sum of zeros, which has no weight in the sum of shares)
+            const float inv_l = it.slot >= 0 && l_run == 0.f ? 1.f : 1.f / l_run, lse = (m_run + log2f(l_run)) * 0.6931471805599453f;
             if (row < tile_rows) {
                 if (it.slot < 0) p.lse[(size_t)h * p.Lq + it.q0 + g * 128 + row] = lse;
                 else p.part_lse[(size_t)h * p.prows + it.slot + g * 128 + row] = lse;

@@ -107,7 +107,7 @@ __global__ void __launch_bounds__(kCrossSoloThreads, 1) cross_solo_tc_kernel(con
             const int id = cross_item(n), rank = id / p.H, h = id - rank * p.H;
             const CrossItem it = p.items[rank];
             if (n + 1 < n_items && lane == 0) prefetch_item(p.items + cross_item(n + 1) / p.H);
-            float m_run = -INFINITY, l_run = 0.f;
+            float m_run = kLowest, l_run = 0.f;
             for (int k = g * 128; k < it.n_keys; k += 256) {
                 const int valid = min(128, it.n_keys - k);
                 ok = mbar_wait_spin(bar(S_FULL + g), n_tile & 1, abort_flag, p.wait, CS_SFULL);
@@ -201,7 +201,7 @@ __global__ void __launch_bounds__(kCrossSoloThreads, 1) cross_solo_tc_kernel(con
                 continue;
             }
             // ---- results of both groups
-            float m1 = -INFINITY, l1 = 0.f;
+            float m1 = kLowest, l1 = 0.f;
             if (both) {
                 ok = mbar_wait(bar(ML), n_ml & 1, abort_flag, p.wait, CS_ML);
                 ok = __all_sync(0xffffffffu, ok);
@@ -210,7 +210,8 @@ __global__ void __launch_bounds__(kCrossSoloThreads, 1) cross_solo_tc_kernel(con
                 l1 = s_ml[1][row];
             }
             const float big = fmaxf(m_run, m1), e0 = ex2(m_run - big), e1 = both ? ex2(m1 - big) : 0.f;
-            const float sum = e0 * l_run + e1 * l1, w0 = e0 / sum, w1 = e1 / sum;
+            // (a share whose states all weigh nothing: its row is a sum of zeros, which has no weight in the sum of shares)
+            const float sum = e0 * l_run + e1 * l1, inv = it.slot >= 0 && sum == 0.f ? 1.f : 1.f / sum, w0 = e0 * inv, w1 = e1 * inv;
             if (row < it.rows) {
                 const float lse = (big + log2f(sum)) * 0.6931471805599453f;
                 if (it.slot < 0) p.lse[(size_t)h * p.Lq + it.q0 + row] = lse;
