@@ -103,3 +103,32 @@ def test_a_value_without_weight_that_is_not_a_number(case):
     channels = torch.arange(d, device="cuda") == 9
     assert bool(torch.isnan(o[:, :q_len[0], channels]).all()) and bool(torch.isfinite(o[:, :, ~channels]).all())
     assert bool(torch.isfinite(o[:, q_len[0]:]).all()) and bool(torch.isfinite(lse).all())
+
+
+@pytest.mark.parametrize("place", PLACES)
+@pytest.mark.parametrize("case", [c for c in CASES if sum(c[5]) < 500])
+def test_gradients_of_states_without_weight(case, place):
+    """dK and dV of a state that weighs nothing are zero (its dP times zero; the queries that a last tile lacks have no part in it), and
+    the others' are as without it.  (dQ is a sum over the states, of which zero times minus infinity is one: NaN by the formula.)"""
+    _, _, H, kv, d, q_len, k_len = case
+    q_off, k_off = _offsets(q_len), _offsets(k_len)
+    q, k, v = _inputs(H, kv, d, q_len, k_len, 6)
+    do = torch.randn(q.shape, generator=torch.Generator("cuda").manual_seed(7), device="cuda").to(torch.bfloat16)
+    gone = torch.zeros(sum(k_len), dtype=torch.bool)
+    for a, n in zip(k_off, k_len):
+        for i in range(n - 1):
+            gone[a + i] = PLACES[place](i, n)
+    k[:, gone, 5] = -float("inf")
+    op = MocCross(H, kv, d, q_off, k_off)
+    ws = op.new_workspace(with_bwd=True)
+    o, lse, dq, dk, dv = torch.empty_like(q), torch.empty(q.shape[:2], device="cuda"), torch.empty_like(q), torch.empty_like(k), torch.empty_like(k)
+    op.moc_cross_attend(q, k, v, o, lse, ws)
+    op.moc_cross_attend_bwd(q, k, v, o, lse, do, dq, dk, dv, ws)
+    torch.cuda.synchronize()
+    assert op.moc_cross_get_status(ws) == (0, 0)
+    keep = ~gone
+    left = [int(keep[a:a + n].sum()) for a, n in zip(k_off, k_len)]
+    ref = R.CrossRef(q.double(), k[:, keep].double(), v[:, keep].double(), q_len, left, _offsets(left)[:-1], d ** -0.5, do.double())
+    R.check("dK", dk[:, keep], ref.dk, ref.dk_tol)
+    R.check("dV", dv[:, keep], ref.dv, ref.dv_tol)
+    assert bool((dk[:, gone] == 0).all()) and bool((dv[:, gone] == 0).all())
