@@ -29,10 +29,14 @@ static int check_cross(const moc_cross_problem *pr) {
     return MOC_OK;
 }
 
-// Shares of the keys.  With many items the longest-first walk balances the CTAs by itself; with few, and long key lists, an item is cut into
-// shares of `c` key tiles, whose results another launch puts together.  c is the one with the least estimated time `t`, in key tiles of
-// two-tile items (3450 cycles): the slowest CTA's walk, where an item costs 0.8 beside its tiles (2800: its first loads and its
-// results) and a key tile of a single query tile `single`, plus `join` for the second launch.
+// Shares of the keys.  With many items of like lengths the longest-first walk balances the CTAs by itself; with few, or with some far longer
+// than the others, an item is cut into shares of `c` key tiles, whose results another launch puts together.  c is the one with the
+// least estimated time `t`, in key tiles of two-tile items (3450 cycles): the slowest CTA's walk, where an item costs 0.8 beside its
+// tiles (2800: its first loads and its results) and a key tile of a single query tile `single`, plus `join` for the second launch.
+// (61 segments of 200 queries, 24 heads of 128, one of them with 32,760 states, the others with 77: forward 151 us and backward 544; with
+// that one's items whole, 24 CTAs on them and the others done, 476 and 710.  All of 512 states, 33k queries: 202 and 650, uncut by either rule.)
+// The costs were measured at d = 128 and are taken for d = 64 too: (12 heads of 64, 40 segments of 700 queries, 38 with 100 states and two
+// with 30,000 and 20,000: forward 377 -> 215 us, backward 672 -> 683.)
 // (No share has more than 16384 key tiles, some 50 ms: a bounded wait lasts a second.)
 constexpr int kMostTiles = 16384;
 struct Shares { int c; double t; };
@@ -44,21 +48,38 @@ static Shares share_tiles(const std::vector<CrossItem> &items, int H, int n_sm, 
         longest = std::max(longest, nt);
         if (nt > 0) total += 0.8 + (i.rows > 128 ? 1.0 : single) * nt;
     }
-    if (items.size() * (size_t)H >= 4 * (size_t)n_sm) return Shares{std::min(longest, kMostTiles), total * H / n_sm};
-    Shares best{longest, 1e300};
+    const double mean = total * H / n_sm;
     std::vector<double> cost;
-    for (int p = 1; p <= std::min(longest, 128); ++p) {
-        const int c = (longest + p - 1) / p;
+    const bool many = items.size() * (size_t)H >= 4 * (size_t)n_sm;
+    // the slowest walk with shares of c tiles, as they are dealt out (cross_item)
+    auto walk = [&](int c) {
         cost.clear();
         for (const CrossItem &i : items) {
             const int nt = (i.n_keys + 127) / 128, n = std::max(1, (nt + c - 1) / c);
             for (int x = 0; x < n && nt > 0; ++x) cost.push_back(0.8 + (i.rows > 128 ? 1.0 : single) * ((int)((int64_t)nt * (x + 1) / n) - (int)((int64_t)nt * x / n)));
         }
         std::sort(cost.begin(), cost.end(), [](double a, double b) { return a > b; });
-        double t = c < longest ? join : 0.0;
-        for (size_t at = 0; at < cost.size() * (size_t)H; at += n_sm) t += cost[at / H];
+        const int64_t n_all = (int64_t)cost.size() * H;
+        double t = 0;
+        for (int b = 0; b < n_sm; ++b) {
+            double mine = 0;
+            for (int64_t at = 0, odd = 0; at < n_all; at += n_sm, odd ^= 1) {
+                const int64_t id = at + (odd ? n_sm - 1 - b : b);
+                if (id < n_all) mine += cost[id / H];
+            }
+            t = std::max(t, mine);
+        }
+        return t;
+    };
+    if (many && walk(longest) <= 1.2 * mean + join) return Shares{std::min(longest, kMostTiles), mean};
+    Shares best{longest, 1e300};
+    // (an item alone may be the whole mean of n_sm CTAs; of many items, each p takes a while)
+    for (int p = 1; p <= std::min(longest, 2 * n_sm); p += many ? 1 + p / 4 : 1) {
+        const int c = (longest + p - 1) / p;
+        const double t = walk(c) + (c < longest ? join : 0.0);
         if (t < best.t) best = Shares{c, t};
-        if (cost.size() * (size_t)H > 4 * (size_t)n_sm) break;   // (shorter shares only cost more)
+        // shorter shares only cost more, unless it is a few long items that they are cut from
+        if (cost.size() * (size_t)H > 4 * (size_t)n_sm && cost[0] <= 0.5 * mean) break;
     }
     best.c = std::min(best.c, kMostTiles);
     return best;
@@ -517,8 +538,25 @@ extern "C" int moc_cross_attend_bwd(const moc_cross *c, const moc_rows *Q, const
     return MOC_OK;
 }
 
+// The key tiles that the CTAs of a launch walk, of the sorted items of every head: the most that one has, and the mean.
+static void walks(const std::vector<CrossItem> &items, int H, int n_sm, int64_t *out) {
+    const int64_t n_all = (int64_t)items.size() * H, n_cta = std::min<int64_t>(n_all, n_sm);
+    out[0] = out[1] = 0;
+    for (int64_t b = 0; b < n_cta; ++b) {
+        int64_t tiles = 0;
+        for (int64_t n = 0; n * n_cta < n_all; ++n) {
+            const int64_t id = n * n_cta + ((n & 1) ? n_cta - 1 - b : b);
+            if (id < n_all) tiles += (items[id / H].n_keys + 127) / 128;
+        }
+        out[0] = std::max(out[0], tiles);
+        out[1] += tiles;
+    }
+    out[1] = n_cta > 0 ? (out[1] + n_cta - 1) / n_cta : 0;
+}
+
 // Test hook, host only: the launches of a problem on a GPU of n_sm SMs.  out: items of the forward's kernels (two query tiles, one, few
-// queries) that have keys, and rows to put together; items of dQ that have keys; pieces of dK/dV; slots of their sums
+// queries) that have keys, and rows to put together; items of dQ that have keys; pieces of dK/dV; slots of their sums; the longest
+// walk and the mean one of the two-tile launch, the one-tile launch and dQ, in key tiles
 extern "C" int moc_debug_cross_plan(const moc_cross_problem *pr, int n_sm, int64_t *out) {
     if (!pr || !out) return MOC_ERR_NULL;
     if (int r = check_cross(pr)) return r;
@@ -533,6 +571,9 @@ extern "C" int moc_debug_cross_plan(const moc_cross_problem *pr, int n_sm, int64
     auto with_keys = [](const std::vector<CrossItem> &items) { return std::count_if(items.begin(), items.end(), [](const CrossItem &i) { return i.n_keys > 0; }); };
     out[0] = with_keys(c.items) * c.H; out[1] = (int64_t)c.solo.size() * c.H; out[2] = (int64_t)c.few.size() * c.Hkv; out[3] = (int64_t)c.prows * c.H;
     out[4] = with_keys(c.dq_items) * c.H; out[5] = (int64_t)c.pieces.size(); out[6] = c.kv_slots;
+    walks(c.items, c.H, n_sm, out + 7);
+    walks(c.solo, c.H, n_sm, out + 9);
+    walks(c.dq_items, c.H, n_sm, out + 11);
     return MOC_OK;
 }
 
