@@ -300,7 +300,9 @@ typedef struct moc_cross_problem {
 
 typedef struct moc_cross moc_cross;
 
-/* As moc_plan_create: validates the tables, derives the work of every launch and uploads it to the current device. */
+/* As moc_plan_create: validates the tables, derives the work of every launch and uploads it to the current device.  Heads x queries,
+ * key heads x states, and the work items and rows of partial results that very long lists are cut into stay below 2^31 - 1024
+ * (MOC_ERR_SHAPE). */
 int moc_cross_create(const moc_cross_problem *problem, moc_cross **out);
 int moc_cross_destroy(moc_cross *cross);
 

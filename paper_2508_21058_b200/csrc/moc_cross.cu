@@ -13,6 +13,9 @@ namespace moc {
 
 static size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
+// Rows, items of all heads, rows of partial results and pieces are counted in 32 bits, some to spare for a tile's last row and a round of items.
+constexpr int64_t kMostCount = (1ll << 31) - 1024;
+
 static int check_cross(const moc_cross_problem *pr) {
     if (pr->n_heads < 1 || pr->n_heads > 65535 || pr->n_kv_heads < 1 || pr->n_heads % pr->n_kv_heads != 0) return MOC_ERR_SHAPE;
     if (pr->head_dim != 64 && pr->head_dim != 128) return MOC_ERR_SHAPE;
@@ -24,8 +27,7 @@ static int check_cross(const moc_cross_problem *pr) {
         if (pr->k_len && (pr->k_len[s] < 0 || pr->k_len[s] > pr->k_off[s + 1] - pr->k_off[s])) return MOC_ERR_CHUNK_TABLE;
     }
     const int64_t Lq = pr->q_off[pr->n_segments], Lk = pr->k_off[pr->n_segments];
-    // (some to spare: a tile's last row, and a round of items, are worked out in 32 bits)
-    if (Lq * pr->n_heads >= (1ll << 31) - 1024 || Lk * pr->n_kv_heads >= (1ll << 31) - 1024) return MOC_ERR_SHAPE;
+    if (Lq * pr->n_heads >= kMostCount || Lk * pr->n_kv_heads >= kMostCount) return MOC_ERR_SHAPE;
     return MOC_OK;
 }
 
@@ -85,8 +87,15 @@ static Shares share_tiles(const std::vector<CrossItem> &items, int H, int n_sm, 
     return best;
 }
 
-// cuts the items into shares of at most c key tiles; the longest items first
-static void cut_items(std::vector<CrossItem> &items, std::vector<CrossMerge> &merges, int &prows, int c) {
+// cuts the items into shares of at most c key tiles; the longest items first.  false: there are more than can be counted
+static bool cut_items(std::vector<CrossItem> &items, std::vector<CrossMerge> &merges, int &prows, int c, int H) {
+    int64_t shares = 0, rows = prows;
+    for (const CrossItem &i : items) {
+        const int nt = (i.n_keys + 127) / 128, n = std::max(1, (nt + c - 1) / c);
+        shares += n;
+        if (n > 1) rows += (int64_t)n * i.rows;
+    }
+    if (shares * H >= kMostCount || rows >= kMostCount) return false;
     std::vector<CrossItem> out;
     for (const CrossItem &i : items) {
         const int nt = (i.n_keys + 127) / 128, n = std::max(1, (nt + c - 1) / c);
@@ -104,9 +113,10 @@ static void cut_items(std::vector<CrossItem> &items, std::vector<CrossMerge> &me
     }
     std::stable_sort(out.begin(), out.end(), [](const CrossItem &a, const CrossItem &b) { return (a.n_keys + 127) / 128 > (b.n_keys + 127) / 128; });
     items.swap(out);
+    return true;
 }
 
-static void derive_cross(moc_cross *c, const moc_cross_problem *pr) {
+static int derive_cross(moc_cross *c, const moc_cross_problem *pr) {
     const int S = pr->n_segments;
     c->H = pr->n_heads; c->Hkv = pr->n_kv_heads; c->g = pr->n_heads / pr->n_kv_heads; c->d = pr->head_dim;
     c->Lq = pr->q_off[S]; c->Lk = pr->k_off[S];
@@ -140,6 +150,7 @@ static void derive_cross(moc_cross *c, const moc_cross_problem *pr) {
         if (!is_few(s)) continue;
         const int q_len = pr->q_off[s + 1] - pr->q_off[s], rows = q_len * c->g, blocks = (rows + 3) / 4, nk = keys(s);
         const int n = (int)((nk + few_share - 1) / few_share);
+        if (((int64_t)c->few.size() + (int64_t)n * blocks) * c->Hkv >= kMostCount || c->prows + (int64_t)n * q_len >= kMostCount) return MOC_ERR_SHAPE;
         for (int x = 0; x < n; ++x) {
             const int k0 = (int)((int64_t)nk * x / n), k1 = (int)((int64_t)nk * (x + 1) / n);
             for (int b = 0; b < blocks; ++b) {
@@ -183,18 +194,18 @@ static void derive_cross(moc_cross *c, const moc_cross_problem *pr) {
     Shares cut = together;
     if (halves.t < std::min(together.t, apart)) {
         c->solo.swap(half);
-        cut_items(c->solo, c->merges, c->prows, halves.c);
+        if (!cut_items(c->solo, c->merges, c->prows, halves.c, c->H)) return MOC_ERR_SHAPE;
     } else if (apart < together.t) {
         c->items.swap(two);
         c->solo.swap(one);
-        cut_items(c->solo, c->merges, c->prows, singles.c);
+        if (!cut_items(c->solo, c->merges, c->prows, singles.c, c->H)) return MOC_ERR_SHAPE;
         cut = pairs;
     } else {
         c->items.swap(both);
     }
     c->items.insert(c->items.end(), none.begin(), none.end());
-    cut_items(c->items, c->merges, c->prows, cut.c);
-    cut_items(c->dq_items, c->dq_merges, c->dq_prows, share_tiles(c->dq_items, c->H, c->n_sm, 1.0, 3.0).c);
+    if (!cut_items(c->items, c->merges, c->prows, cut.c, c->H)) return MOC_ERR_SHAPE;
+    if (!cut_items(c->dq_items, c->dq_merges, c->dq_prows, share_tiles(c->dq_items, c->H, c->n_sm, 1.0, 3.0).c, c->H)) return MOC_ERR_SHAPE;
     for (const CrossMerge &m : c->merges) {
         c->most_merge_rows = std::max(c->most_merge_rows, m.rows);
         c->most_merge_n = std::max(c->most_merge_n, m.n);
@@ -238,6 +249,9 @@ static void derive_cross(moc_cross *c, const moc_cross_problem *pr) {
         if (at > 64ll * c->n_sm) break;                              // (shorter parts only cost more)
     }
     part = std::min<int64_t>(part, 1 << 16);                         // (a bounded wait lasts a second, as long as 500000 pairs)
+    int64_t n_pieces = 0;
+    for (const Group &g : groups) n_pieces += (g.units + part - 1) / part * g.n;
+    if (n_pieces >= kMostCount) return MOC_ERR_SHAPE;
     std::vector<CrossPiece> all;
     for (const Group &g : groups) {
         const int64_t parts = (g.units + part - 1) / part;
@@ -271,6 +285,7 @@ static void derive_cross(moc_cross *c, const moc_cross_problem *pr) {
     w.part_dq = up256(w.delta + 4 * H * c->Lq);
     w.part_kv = up256(w.part_dq + 4 * H * c->dq_prows * d);
     w.bwd_end = up256(w.part_kv + 4 * 2 * (size_t)c->kv_slots * 128 * d);
+    return MOC_OK;
 }
 
 // The launches that put shares together begin while the one before them still runs, and wait for its results.
@@ -403,7 +418,10 @@ extern "C" int moc_cross_create(const moc_cross_problem *pr, moc_cross **out) {
     c->device = dev;
     c->n_sm = n_sm;
     try {                                                       // (the tables' memory)
-        derive_cross(c, pr);
+        if (int r = derive_cross(c, pr)) {
+            delete c;
+            return r;
+        }
         size_t o = 0;
         auto take = [&](size_t bytes) { const size_t at = o; o = up256(o + bytes); return at; };
         const size_t a = take(sizeof(CrossItem) * c->items.size()), b = take(sizeof(CrossItem) * c->dq_items.size()),
@@ -564,7 +582,7 @@ extern "C" int moc_debug_cross_plan(const moc_cross_problem *pr, int n_sm, int64
     moc_cross c = {};
     c.n_sm = n_sm;
     try {
-        derive_cross(&c, pr);
+        if (int r = derive_cross(&c, pr)) return r;
     } catch (...) {
         return MOC_ERR_CUDA;
     }

@@ -3,6 +3,7 @@ import random
 
 import pytest
 
+from paper_2508_21058_b200 import MocError
 from paper_2508_21058_b200.binding import debug_cross_plan
 
 N_SM = 148
@@ -57,3 +58,15 @@ def test_walks_of_any_lists():
         for launch in ("two_tile", "one_tile", "dq"):
             assert p[launch + "_walk"] <= 2 * p[launch + "_mean"] + 16, (heads, kv, q, k, launch, p)
     assert cut > 50
+
+
+@pytest.mark.parametrize("case", [
+    (1, 1, 64, [5_000_000], [2**30]),                # 512 shares of 5M rows
+    (1, 1, 64, [2**23, 2**23], [2**29, 2**29 + 5]),
+])
+def test_more_than_can_be_counted_is_refused(case):
+    """Rows of partial results and work items are 32-bit numbers: a plan with more is refused before anything is allocated for it."""
+    with pytest.raises(MocError) as e:
+        plan(*case)
+    assert e.value.code == -2
+    assert plan(*case[:3], [300] * len(case[4]), case[4])["part_rows"] > 0
