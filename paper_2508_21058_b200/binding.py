@@ -320,7 +320,7 @@ class MocRope:
     def __init__(self, head_dim, pair_axis=(), pair_freq=(), n_axes=None, eps=1e-6, halves=False):
         self._lib = load_library()
         self._h = C.c_void_p(0)
-        axis = np.ascontiguousarray(pair_axis, np.int32)
+        axis = _int32(pair_axis, "pair_axis")
         freq = np.ascontiguousarray(pair_freq, np.float64)
         if axis.shape != freq.shape or axis.ndim != 1:
             raise MocError(-2, "moc error -2: pair_axis and pair_freq are lists of the same length")
@@ -397,10 +397,18 @@ class MocRope:
             _check(code)
 
 
+def _int32(values, name):
+    """A table of whole numbers for the library; one that does not fit is refused, where a cast would wrap or cut it."""
+    t = np.asarray(values)
+    if t.size and (t.dtype.kind not in "biuf" or not (t.min() >= -2**31 and t.max() < 2**31) or (t != np.floor(t)).any()):
+        raise MocError(-2, f"moc error -2: {name} is a list of whole numbers below 2^31")
+    return np.ascontiguousarray(t, np.int32)
+
+
 def _cross_problem(n_heads, n_kv_heads, head_dim, q_off, k_off, k_len, softmax_scale):
     """The C problem statement, and the host arrays it points to."""
-    qo, ko = np.ascontiguousarray(q_off, np.int32), np.ascontiguousarray(k_off, np.int32)
-    kl = None if k_len is None else np.ascontiguousarray(k_len, np.int32)
+    qo, ko = _int32(q_off, "q_off"), _int32(k_off, "k_off")
+    kl = None if k_len is None else _int32(k_len, "k_len")
     if qo.ndim != 1 or len(qo) < 1 or ko.shape != qo.shape or (kl is not None and kl.shape != (len(qo) - 1,)):
         raise MocError(-3, "moc error -3: segment tables have inconsistent lengths")
     pr = _CrossProblem(int(n_heads), int(n_kv_heads), int(head_dim), len(qo) - 1, float(softmax_scale), qo.ctypes.data, ko.ctypes.data,
