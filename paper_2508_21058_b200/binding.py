@@ -94,6 +94,7 @@ def load_library():
     lib.moc_cross_attend.argtypes = [vp] + [rows] * 4 + [vp] * 3
     lib.moc_cross_attend_bwd.argtypes = [vp] + [rows] * 4 + [vp] + [rows] * 4 + [vp] * 2
     lib.moc_cross_get_status.argtypes = [vp, vp, vp, C.POINTER(i32), C.POINTER(i32)]
+    lib.moc_debug_rope_split.argtypes = [i32, i32, i32, C.c_int64, i32, i32, i32, C.POINTER(C.c_int64)]
     lib.moc_debug_cross_plan.argtypes = [C.POINTER(_CrossProblem), i32, C.POINTER(C.c_int64)]
     lib.moc_selected_pairs.argtypes = [vp, vp, vp, C.POINTER(C.c_int64)]
     lib.moc_get_status.argtypes = [vp, vp, vp, C.POINTER(i32), C.POINTER(i32)]
@@ -308,6 +309,13 @@ def _scratch(ws, n_bytes, dev):
         raise MocError(-5, f"moc error -5: a contiguous workspace of {n_bytes} bytes is needed")
     _on_current(ws, "the workspace", dev)
     return ws.data_ptr()
+
+
+def debug_rope_split(fp32, bwd, head_dim, n_tokens, n_q, n_k, n_sm=148):
+    """Test hook, host only: how a call of MocRope deals out its work on n_sm SMs."""
+    out = (C.c_int64 * 7)()
+    _check(load_library().moc_debug_rope_split(int(fp32), int(bwd), int(head_dim), int(n_tokens), int(n_q), int(n_k), int(n_sm), out))
+    return dict(zip(("by_token", "q_units", "k_units", "per_warp", "n_split", "items", "warps"), out))
 
 
 class MocRope:

@@ -386,20 +386,45 @@ __global__ void __launch_bounds__(1024) norm_rope_dw_kernel(const float *part, i
 // the most blocks that a backward launch has: what the workspace holds sums of
 constexpr int kRopeMaxBlocks = 2048;
 
-template <int D, bool HALVES, bool FULL, bool BY_TOKEN, typename X, bool BWD>
-static int launch_norm_rope_u(const moc_rope *r, RopeParams &a, float *dw_q, float *dw_k, int n_sm, cudaStream_t s) {
-    using RB = RopeBatch<X, BWD>;
-    constexpr int RPW = 32 / (D / 8), batch = RB::U * (BY_TOKEN ? 1 : RPW), per_sm = RB::BLOCKS;      // heads of a batch
-    for (int z = 0; z < 2; ++z) a.units[z] = (a.side[z].heads + batch - 1) / batch;
-    const int units = a.units[0] + a.units[1];
+// How a launch deals out a stream's heads: batches that a token's heads make, batches a warp takes and warps that share a token (groups of
+// tokens: those of a warp), and blocks.
+struct RopeSplit {
+    bool by_token;
+    int units[2], per_warp, n_split;
+    int64_t items;
+    unsigned grid;
+};
+// The lane groups of a warp have heads of one token in turn, next to one another in a projection; or, where that leaves more lanes without a
+// row, a token each.  (33k tokens, bf16, forward and backward, heads of one token and a token each: 12 + 12 heads of 128 70 / 122 and
+// 73 / 120 us; 66k tokens, 6 + 2 heads of 64, 71 / 118 and 34 / 54; 264k tokens, 1 + 1 head of 128, 248 / 396 and 132 / 210.  An fp32
+// projection, 6.4k tokens, 24 + 24 heads of 128, 40 / 70 and 43 / 80.  With the step from head to head as an argument of one kernel
+// instead, the same cases were 77 / 138, 37 / 57 and 153 / 255.)
+static RopeSplit split_norm_rope(bool fp32, bool bwd, int d, int64_t n_tokens, const int (&heads)[2], int n_sm) {
+    const int U = fp32 ? RopeBatch<float, false>::U : RopeBatch<__nv_bfloat16, false>::U, rpw = 32 / (d / 8);
+    const int per_sm = bwd ? RopeBatch<float, true>::BLOCKS : RopeBatch<float, false>::BLOCKS;
+    int in_turn = 0, a_token = 0;                               // rows that a lane group has room for, at a token
+    for (int h : heads) {
+        in_turn += (h + U * rpw - 1) / (U * rpw) * rpw;
+        a_token += (h + U - 1) / U;
+    }
+    RopeSplit p;
+    p.by_token = a_token < in_turn;
+    const int batch = U * (p.by_token ? 1 : rpw);               // heads of a batch
+    for (int z = 0; z < 2; ++z) p.units[z] = (heads[z] + batch - 1) / batch;
+    const int units = p.units[0] + p.units[1];
     // A warp takes all of its tokens' heads, unless that leaves warps without work: then as many batches of heads as give every warp
     // one (each forms the angles of its tokens again).
-    const int64_t warps = (int64_t)n_sm * per_sm * kRopeWarps, groups = BY_TOKEN ? ((int64_t)a.n_tokens + RPW - 1) / RPW : a.n_tokens;
-    int split = (int)std::min<int64_t>(units, (warps + groups - 1) / groups);
-    a.per_warp = (units + split - 1) / split;
-    a.n_split = (units + a.per_warp - 1) / a.per_warp;
-    const int64_t items = groups * a.n_split;
-    const unsigned grid = (unsigned)std::min<int64_t>({(items + kRopeWarps - 1) / kRopeWarps, (int64_t)n_sm * per_sm, (int64_t)kRopeMaxBlocks});
+    const int64_t warps = (int64_t)n_sm * per_sm * kRopeWarps, groups = p.by_token ? (n_tokens + rpw - 1) / rpw : n_tokens;
+    const int split = (int)std::min<int64_t>(units, (warps + groups - 1) / groups);
+    p.per_warp = (units + split - 1) / split;
+    p.n_split = (units + p.per_warp - 1) / p.per_warp;
+    p.items = groups * p.n_split;
+    p.grid = (unsigned)std::min<int64_t>({(p.items + kRopeWarps - 1) / kRopeWarps, (int64_t)n_sm * per_sm, (int64_t)kRopeMaxBlocks});
+    return p;
+}
+
+template <int D, bool HALVES, bool FULL, bool BY_TOKEN, typename X, bool BWD>
+static int launch_norm_rope_u(const moc_rope *r, const RopeParams &a, unsigned grid, float *dw_q, float *dw_k, cudaStream_t s) {
     norm_rope_kernel<D, HALVES, FULL, BY_TOKEN, X, BWD><<<grid, kRopeWarps * 32, 0, s>>>(r->tab, a);
     MOC_LAUNCH_CHECK();
     if (BWD && (dw_q || dw_k)) {
@@ -409,21 +434,14 @@ static int launch_norm_rope_u(const moc_rope *r, RopeParams &a, float *dw_q, flo
     return MOC_OK;
 }
 
-// The lane groups of a warp have heads of one token in turn, next to one another in a projection; or, where that leaves more lanes without a
-// row, a token each.  (33k tokens, bf16, forward and backward, heads of one token and a token each: 12 + 12 heads of 128 70 / 122 and
-// 73 / 120 us; 66k tokens, 6 + 2 heads of 64, 71 / 118 and 34 / 54; 264k tokens, 1 + 1 head of 128, 248 / 396 and 132 / 210.  An fp32
-// projection, 6.4k tokens, 24 + 24 heads of 128, 40 / 70 and 43 / 80.  With the step from head to head as an argument of one kernel
-// instead, the same cases were 77 / 138, 37 / 57 and 153 / 255.)
 template <int D, bool HALVES, bool FULL, typename X, bool BWD>
 static int launch_norm_rope_t(const moc_rope *r, RopeParams &a, float *dw_q, float *dw_k, int n_sm, cudaStream_t s) {
-    constexpr int U = RopeBatch<X, BWD>::U, RPW = 32 / (D / 8);
-    int in_turn = 0, a_token = 0;                               // rows that a lane group has room for, at a token
-    for (const RopeSide &sd : a.side) {
-        in_turn += (sd.heads + U * RPW - 1) / (U * RPW) * RPW;
-        a_token += (sd.heads + U - 1) / U;
-    }
-    return a_token < in_turn ? launch_norm_rope_u<D, HALVES, FULL, true, X, BWD>(r, a, dw_q, dw_k, n_sm, s)
-                             : launch_norm_rope_u<D, HALVES, FULL, false, X, BWD>(r, a, dw_q, dw_k, n_sm, s);
+    const RopeSplit p = split_norm_rope(sizeof(X) == 4, BWD, D, a.n_tokens, {a.side[0].heads, a.side[1].heads}, n_sm);
+    for (int z = 0; z < 2; ++z) a.units[z] = p.units[z];
+    a.per_warp = p.per_warp;
+    a.n_split = p.n_split;
+    return p.by_token ? launch_norm_rope_u<D, HALVES, FULL, true, X, BWD>(r, a, p.grid, dw_q, dw_k, s)
+                      : launch_norm_rope_u<D, HALVES, FULL, false, X, BWD>(r, a, p.grid, dw_q, dw_k, s);
 }
 
 template <bool BWD>
@@ -565,4 +583,15 @@ extern "C" int moc_norm_rope_bwd(const moc_rope *r, int x_type, int32_t n_tokens
     if (!aligned(ws, 256)) return MOC_ERR_ALIGN;
     a.part = static_cast<float *>(ws);
     return launch_norm_rope<true>(r, a, x_type, dw[0], dw[1], (cudaStream_t)stream);
+}
+
+// Test hook, host only: how the launch of a call on n_sm SMs deals out its work.  out: a token for each lane group, batches of queries and
+// of keys, batches a warp takes, warps that share a token, items, warps
+extern "C" int moc_debug_rope_split(int x_type, int bwd, int d, int64_t n_tokens, int n_q, int n_k, int n_sm, int64_t *out) {
+    if (!out) return MOC_ERR_NULL;
+    if ((x_type != MOC_BF16 && x_type != MOC_FP32) || (d != 64 && d != 128) || n_tokens < 1 || n_q < 1 || n_k < 0 || n_sm < 1) return MOC_ERR_SHAPE;
+    const RopeSplit p = split_norm_rope(x_type == MOC_FP32, bwd != 0, d, n_tokens, {n_q, n_k}, n_sm);
+    const int64_t v[7] = {p.by_token, p.units[0], p.units[1], p.per_warp, p.n_split, p.items, (int64_t)p.grid * kRopeWarps};
+    std::copy(v, v + 7, out);
+    return MOC_OK;
 }
