@@ -278,6 +278,8 @@ class MocPlan:
 
 def _rows(t, heads, tokens, d, dtype, name, dev, spare=False):
     """A [heads][tokens][d] tensor of any strides as the library takes it; `spare`: it may have more tokens."""
+    if t is None:
+        raise MocError(-1, f"moc error -1: {name} is missing")
     shape = t.shape
     if t.dtype is dtype and t.get_device() == dev and len(shape) == 3 and shape[0] == heads and shape[2] == d and (
             shape[1] == tokens or (spare and shape[1] > tokens)):
@@ -369,6 +371,8 @@ class MocRope:
         return torch.empty(self._ws_bytes, dtype=torch.uint8, device=device)
 
     def _common(self, pos, q, k, dev):
+        if q is None:
+            raise MocError(-1, "moc error -1: q is missing")
         if q.dim() != 3 or q.dtype not in (torch.bfloat16, torch.float32):
             raise MocError(-2, f"moc error -2: queries are [head][token][d], bf16 or fp32, not {q.dtype} {tuple(q.shape)}")
         if k is not None and k.dim() != 3:

@@ -1,10 +1,11 @@
-"""Tables that the binding hands to the library: whole numbers that fit, or refused; a cast would wrap or cut them without a word."""
+"""What the binding hands to the library: tables of whole numbers that fit, or refused, where a cast would wrap or cut them without a word;
+tensors that are missing are refused as the library does it."""
 import numpy as np
 import pytest
 import torch
 
 from paper_2508_21058_b200 import MocCross, MocError, MocRope
-from paper_2508_21058_b200.binding import debug_cross_plan
+from paper_2508_21058_b200.binding import _rows, debug_cross_plan
 
 WRAPS = np.array([0, 2**32 + 5])
 
@@ -34,3 +35,12 @@ def test_axes_of_a_rotation():
         with pytest.raises(MocError) as e:
             MocRope(64, axis, [1.0, 2.0])
         assert e.value.code == -2
+
+
+def test_a_missing_tensor():
+    with pytest.raises(MocError) as e:
+        _rows(None, 2, 3, 64, torch.bfloat16, "k_out", 0)
+    assert e.value.code == -1
+    with pytest.raises(MocError) as e:
+        MocRope(64)._common(None, None, None, 0)
+    assert e.value.code == -1
