@@ -231,7 +231,8 @@ int moc_outer_reduced_layout(const moc_plan *plan, const int32_t *sel_shot, int3
 int moc_gather_tokens(const moc_plan *plan, const void *X, const int32_t *tok_map, int32_t n_out, void *out, void *stream);
 
 /* ---- Beside the stream's sparse attention: what a layer does to its queries and keys before it, and the cross attention behind
- * it (the DiT block of the paper's experiments: Wan-2.1 style per-head norm, 3-D rotary positions, cross attention to the prompt).
+ * it: a norm of every head's row, 3-D rotary positions, cross attention to the prompt.  (The norm is a head's own, with one weight for all
+ * heads.  Models that norm a token's whole row before it is cut into heads, as Wan-2.1 does, do that themselves, and take the rotation alone.)
  *
  * Rows of d consecutive values, one per (head, token): row (h, t) begins at data + h * head_stride + t * token_stride elements.
  * data is a DEVICE pointer, 16-byte aligned; both strides are multiples of 16 bytes, below 2^39 elements, and keep the rows apart:
@@ -271,7 +272,8 @@ int moc_rope_workspace_bytes(const moc_rope *rope, size_t *bytes);     /* for mo
  *     u = x / sqrt(mean(x^2) + eps) * w  (w NULL: u = x),  out = the rotation of u by the token's angles, rounded once to bf16.
  * x_type (MOC_BF16, MOC_FP32) is the type of q and k; q_out, k_out are bf16, in the layout that moc_chunk_pool / moc_route /
  * moc_attend take when they are contiguous [H][L][d].  w_q, w_k: DEVICE fp32 [d], shared by all heads.  pos: DEVICE int32
- * [n_tokens][n_axes] (any value; angles are formed in 64 bits).  n_k_heads may be 0: k, w_k, k_out are not looked at then.  n_tokens may be 0.
+ * [n_tokens][n_axes] (any value; an angle of a radians is formed in 64 bits, off by some |a| 2^-52, and reduced before it is rounded
+ * to fp32).  n_k_heads may be 0: k, w_k, k_out are not looked at then.  n_tokens may be 0.
  * Squares are summed in fp32: rows of values beyond 1e18, or without an eps below 1e-19, leave its range.
  * An output may be its own input where type and strides are the same; no other overlap. */
 int moc_norm_rope(const moc_rope *rope, int x_type, int32_t n_tokens, int32_t n_q_heads, int32_t n_k_heads, const int32_t *pos,
@@ -321,7 +323,7 @@ int moc_cross_attend(const moc_cross *cross, const moc_rows *Q, const moc_rows *
 
 /* Its backward pass: dQ, dK, dV (bf16) from dO; the gradients of shared key heads are summed over their query heads, in an order that
  * depends on the problem alone.  Padding, and states whose segment has no queries, get zeros.  P and dS are rounded to bf16 before
- * their contractions, as in moc_attend_bwd. */
+ * their contractions, as in moc_attend_bwd.  dQ, dK and dV overlap no other tensor of the call. */
 int moc_cross_attend_bwd(const moc_cross *cross, const moc_rows *Q, const moc_rows *K, const moc_rows *V, const moc_rows *O,
                          const float *lse, const moc_rows *dO, const moc_rows *dQ, const moc_rows *dK, const moc_rows *dV, void *ws,
                          void *stream);

@@ -305,4 +305,7 @@ int moc_debug_wait_probe(const moc_plan *plan, void *ws, int code, void *stream)
 // host only: the long key tiles of dK/dV of a problem on a GPU with n_sm SMs (up to cap of them written): tiles of query rows that
 // a tile has whatever is picked, and blocks that share them; and the bytes there are for the counters of all heads' tiles
 int moc_debug_shared_key_tiles(const moc_problem *problem, int n_sm, int cap, int *n_tiles, int *query_tiles, int *blocks, size_t *counter_room);
+// host only: what a cross attention launches (moc_cross.cu), and how a norm and rotation deals out its heads (moc_norm_rope.cu)
+int moc_debug_cross_plan(const moc_cross_problem *problem, int n_sm, int64_t *out);
+int moc_debug_rope_split(int x_type, int bwd, int d, int64_t n_tokens, int n_q, int n_k, int n_sm, int64_t *out);
 }

@@ -210,7 +210,6 @@ static int derive_cross(moc_cross *c, const moc_cross_problem *pr) {
         c->most_merge_rows = std::max(c->most_merge_rows, m.rows);
         c->most_merge_n = std::max(c->most_merge_n, m.n);
     }
-    for (const CrossItem &i : c->items) c->n_work += i.n_keys > 0;
     for (const CrossItem &i : c->dq_items) c->n_dq_work += i.n_keys > 0;
 
     // Key-stationary pass.  The query tiles of a (key head, segment) are cut into parts of about the same length, and every key tile of
@@ -219,13 +218,12 @@ static int derive_cross(moc_cross *c, const moc_cross_problem *pr) {
     // of the stream: 33k queries, 512 states, 24 heads 340 us and 1.6 GB from DRAM; so 331 us and 0.42 GB).
     struct Group { int h, s; int64_t units; int n; };                // pairs of a key tile; pieces of a part
     std::vector<Group> groups;
-    int64_t total = 0, longest = 0;
+    int64_t longest = 0;
     for (int h = 0; h < c->Hkv; ++h)
         for (int s = 0; s < S; ++s) {
             const int64_t units = (int64_t)c->g * ((pr->q_off[s + 1] - pr->q_off[s] + 127) / 128);
             const int nk = units == 0 ? 0 : keys(s);                 // states that somebody reads
             if (nk > 0) groups.push_back(Group{h, s, units, (nk + 127) / 128});
-            total += units * ((nk + 127) / 128);
             if (nk > 0) longest = std::max(longest, units);
             for (int k = pr->k_off[s] + nk; k < pr->k_off[s + 1]; k += 128)
                 c->sums.push_back(CrossSum{h, k, std::min(128, pr->k_off[s + 1] - k), 0, 0, {}});

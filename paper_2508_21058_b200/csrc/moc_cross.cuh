@@ -26,7 +26,10 @@ constexpr int kCrossRows = 256;
 // of minus infinity.
 constexpr float kLowest = -3.402823466e38f;
 
-constexpr int kFewRows = 8;        // rows of a key head up to which a segment counts as one with few queries
+// Rows of a key head up to which a segment counts as one with few queries.  Not a measured crossover: 64 segments of one query and 1500
+// states take 77 us with three rows a key head there (24 heads on 8), and 163 with 12 or 24 (on 2 or 1) on the tensor cores, where each
+// query head has a tile of its own; neither was tried the other way.
+constexpr int kFewRows = 8;
 
 struct CrossLayout {
     size_t status;
@@ -52,7 +55,7 @@ struct moc_cross {
     int few_rows = 0;                                  // the most rows that one has
     int most_merge_rows = 0, most_merge_n = 0;         // of the forward's merges
     int prows = 0, dq_prows = 0, kv_slots = 0;         // rows of partial results of a head, the same of dQ; slots in all
-    int n_work = 0, n_dq_work = 0;                     // items that have keys: the others, which come last, only need zeros
+    int n_dq_work = 0;                                 // dQ's items that have keys: the others, which come last, only need zeros
     void *d_blob = nullptr;
     moc::CrossItem *d_items, *d_solo, *d_dq_items;
     moc::CrossFew *d_few;

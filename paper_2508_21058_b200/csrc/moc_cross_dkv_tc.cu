@@ -5,15 +5,16 @@
 //     threads (two per TMEM lane) turn T1 into P, then (P, T2) into dS, written back to TMEM as bf16
 //     ACC1 += dS Q,  ACC2 += P dO   (A from TMEM, the streamed tile as an MN-major operand)
 //
-// There are few key tiles (a prompt has some 500 states) and many query tiles, whose products are all alike: the plan puts all
-// (key tile, query tile) pairs in a row and cuts it into equal stretches, one for each CTA.  A stretch is a few pieces, each of one key
-// tile; where a key tile lies in several stretches, each leaves its fp32 sums and another launch adds them up in their order.  A shared
-// key head's query heads are just more query tiles of the same key tile.
+// There are few key tiles (a prompt has some 500 states) and many query tiles, whose products are all alike: the plan cuts the query tiles of
+// a key head and segment into parts of about the same length, and a piece is one key tile against one part.  The pieces of a part follow one another in
+// the list that is dealt out to the CTAs, so that neighbours stream the same queries, out of L2.  Where a key tile has several parts, each
+// leaves its fp32 sums in a slot and another launch adds them up in their order.  A shared key head's query heads are just more
+// query tiles of the same key tile.
 // A CTA holds the piece's 128 keys (K, V) and streams (Q, dO), 128 rows at a time, through rings of three and two stages that run
 // across pieces.  Issue order: ACC2(j), T1(j+1), ACC1(j), T2(j+1): while the lanes form P(j+1) the pipe runs ACC1(j) and T2(j+1).
 // 16 warps: 0-7 the lane threads, 8-11 the producers (two for each ring), 12 and 13 the MMA issuers, 14 the key tiles, 15 idle.
-// 33k queries, 512 states, 24 heads of 128: 331 us, 1260 TFLOP/s; a pair of tiles takes 3100 cycles, of which its products are 2048: the
-// lanes' way from T1 and T2 to dS bounds it.
+// 33k queries, 512 states, 24 heads of 128: 312 to 345 us, up to 1330 TFLOP/s (by the clock that the power cap leaves).
+// A pair of tiles takes 3100 cycles, of which its products are 2048: the lanes' way from T1 and T2 to dS bounds it.
 #include <algorithm>
 
 #include "moc_cross.cuh"

@@ -15,8 +15,8 @@
 //   warps 10, 11, 14, 15  its delta, 32 rows each;
 //   warps 12,13 MMA issuers: warp 12 T1, warp 13 T2 and ACC.  T1(j + 1) is issued once the lanes have read T1(j), T2(j + 2)
 //               after ACC(j), which reads the dS over T2(j).
-// 33k queries, 512 states, 24 heads of 128: 312 us, 1000 TFLOP/s.  A pair of tiles takes 2700 cycles in a row and 400 more shared out
-// from between items: the chain T1 -> P -> dS -> ACC of a tile bounds it (without the loads of K, V, Q and dO 14 % less).
+// 33k queries, 512 states, 24 heads of 128: 300 to 335 us, up to 1040 TFLOP/s (by the clock that the power cap leaves).
+// A pair of tiles takes 2700 cycles in a row and 400 more shared out from between items: the chain T1 -> P -> dS -> ACC of a tile bounds it (without the loads of K, V, Q and dO 14 % less).
 #include <algorithm>
 
 #include "moc_cross.cuh"

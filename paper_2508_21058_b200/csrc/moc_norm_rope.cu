@@ -394,8 +394,9 @@ struct RopeSplit {
     int64_t items;
     unsigned grid;
 };
-// The lane groups of a warp have heads of one token in turn, next to one another in a projection; or, where that leaves more lanes without a
-// row, a token each.  (33k tokens, bf16, forward and backward, heads of one token and a token each: 12 + 12 heads of 128 70 / 122 and
+// The lane groups of a warp have heads of one token in turn, next to one another in a projection; or a token each, where that has room for fewer
+// rows.  Room is counted in whole batches, although rows that no lane has cost nothing: 16 + 16 and 40 + 40 heads of 128 go by token too, where in
+// turn no lane would be without a row either (33k tokens 94 / 153 and 231 / 351 us, 1.12 to 1.24 times the copy's; in turn not timed).  (33k tokens, bf16, forward and backward, heads of one token and a token each: 12 + 12 heads of 128 70 / 122 and
 // 73 / 120 us; 66k tokens, 6 + 2 heads of 64, 71 / 118 and 34 / 54; 264k tokens, 1 + 1 head of 128, 248 / 396 and 132 / 210.  An fp32
 // projection, 6.4k tokens, 24 + 24 heads of 128, 40 / 70 and 43 / 80.  With the step from head to head as an argument of one kernel
 // instead, the same cases were 77 / 138, 37 / 57 and 153 / 255.)
@@ -413,7 +414,8 @@ static RopeSplit split_norm_rope(bool fp32, bool bwd, int d, int64_t n_tokens, c
     for (int z = 0; z < 2; ++z) p.units[z] = (heads[z] + batch - 1) / batch;
     const int units = p.units[0] + p.units[1];
     // A warp takes all of its tokens' heads, unless that leaves warps without work: then as many batches of heads as give every warp
-    // one (each forms the angles of its tokens again).
+    // one (each forms the angles of its tokens again).  The longest warp is not looked at: 1,601 groups of three batches for 2,368 warps
+    // (6.4k tokens, 12 + 4 heads of 64, backward) are cut in two, and some warps have four batches.
     const int64_t warps = (int64_t)n_sm * per_sm * kRopeWarps, groups = p.by_token ? (n_tokens + rpw - 1) / rpw : n_tokens;
     const int split = (int)std::min<int64_t>(units, (warps + groups - 1) / groups);
     p.per_warp = (units + split - 1) / split;
