@@ -493,9 +493,10 @@ int prepare_cross_dq(moc_cross *c) {
 template <int D>
 static int cross_dq_d(const moc_cross *c, const moc_rows *Q, const moc_rows *K, const moc_rows *V, const moc_rows *O, const float *lse, const moc_rows *dO,
                       const moc_rows *dQ, void *ws, cudaStream_t s) {
-    CUtensorMap tmQ = {}, tmdO = {}, tmK = {}, tmV = {}, tmK16 = {}, tmV16 = {};
+    CUtensorMap tmQ, tmdO, tmK, tmV, tmK16, tmV16;
     if (int r = make_tmap_rows_bf16(&tmQ, Q, c->H, c->Lq, D, 128)) return r;
     if (int r = make_tmap_rows_bf16(&tmdO, dO, c->H, c->Lq, D, 128)) return r;
+    tmK = tmV = tmK16 = tmV16 = tmQ;                     // (without any states no key tile is loaded, but the maps are asked for ahead)
     if (c->Lk > 0) {
         if (int r = make_tmap_rows_bf16(&tmK, K, c->Hkv, c->Lk, D, 128)) return r;
         if (int r = make_tmap_rows_bf16(&tmV, V, c->Hkv, c->Lk, D, 128)) return r;

@@ -483,9 +483,10 @@ int prepare_cross_fwd(moc_cross *c) {
 template <int D>
 static int cross_fwd_d(const moc_cross *c, const moc_rows *Q, const moc_rows *K, const moc_rows *V, const moc_rows *O, float *lse, void *ws,
                        bool first, cudaStream_t s) {
-    CUtensorMap tmQ = {}, tmK = {}, tmV = {}, tmK16 = {}, tmV16 = {};
+    CUtensorMap tmQ, tmK, tmV, tmK16, tmV16;
     if (int r = make_tmap_rows_bf16(&tmQ, Q, c->H, c->Lq, D, 128)) return r;
-    if (c->Lk > 0) {                                     // (without any states no key tile is loaded)
+    tmK = tmV = tmK16 = tmV16 = tmQ;                     // (without any states no key tile is loaded, but the maps are asked for ahead)
+    if (c->Lk > 0) {
         if (int r = make_tmap_rows_bf16(&tmK, K, c->Hkv, c->Lk, D, 128)) return r;
         if (int r = make_tmap_rows_bf16(&tmV, V, c->Hkv, c->Lk, D, 128)) return r;
         if (int r = make_tmap_rows_bf16(&tmK16, K, c->Hkv, c->Lk, D, 16)) return r;
