@@ -432,10 +432,10 @@ def debug_cross_plan(n_heads, n_kv_heads, head_dim, q_off, k_off, k_len=None, n_
     """Test hook, host only: what MocCross of the same arguments launches on n_sm SMs: items of the forward's three kernels, rows of
     partial results, items of dQ, pieces of dK/dV and slots of their sums; key tiles that a CTA walks at most and in the mean."""
     pr, tables = _cross_problem(n_heads, n_kv_heads, head_dim, q_off, k_off, k_len, 0.0)
-    out = (C.c_int64 * 13)()
+    out = (C.c_int64 * 14)()
     _check(load_library().moc_debug_cross_plan(C.byref(pr), int(n_sm), out))
     return dict(zip(("two_tile", "one_tile", "few", "part_rows", "dq", "pieces", "slots", "two_tile_walk", "two_tile_mean", "one_tile_walk",
-                     "one_tile_mean", "dq_walk", "dq_mean"), out))
+                     "one_tile_mean", "dq_walk", "dq_mean", "two_tile_wait"), out))
 
 
 class MocCross:

@@ -205,6 +205,11 @@ static int derive_cross(moc_cross *c, const moc_cross_problem *pr) {
     }
     c->items.insert(c->items.end(), none.begin(), none.end());
     if (!cut_items(c->items, c->merges, c->prows, cut.c, c->H)) return MOC_ERR_SHAPE;
+    // The second tile's warps wait through a CTA's items of one tile for the next of two, and no longer than two seconds.  Where there are more
+    // than some 0.6 of that (4200 cycles a key tile, at 1.3 GHz), the items of two come first.
+    int64_t ones = 0;
+    for (const CrossItem &i : c->items) ones += i.rows <= 128 ? (i.n_keys + 127) / 128 : 0;
+    if (ones * c->H / c->n_sm > 200000) std::stable_partition(c->items.begin(), c->items.end(), [](const CrossItem &i) { return i.rows > 128; });
     if (!cut_items(c->dq_items, c->dq_merges, c->dq_prows, share_tiles(c->dq_items, c->H, c->n_sm, 1.0, 3.0).c, c->H)) return MOC_ERR_SHAPE;
     for (const CrossMerge &m : c->merges) {
         c->most_merge_rows = std::max(c->most_merge_rows, m.rows);
@@ -570,9 +575,30 @@ static void walks(const std::vector<CrossItem> &items, int H, int n_sm, int64_t 
     out[1] = n_cta > 0 ? (out[1] + n_cta - 1) / n_cta : 0;
 }
 
+// The most key tiles that a CTA of the two-tile launch walks in items of one query tile before one of two, whose second tile's warps wait
+// through them.
+static int64_t longest_wait(const std::vector<CrossItem> &items, int H, int n_sm) {
+    const int64_t n_all = (int64_t)items.size() * H, n_cta = std::min<int64_t>(n_all, n_sm);
+    int64_t most = 0;
+    for (int64_t b = 0; b < n_cta; ++b) {
+        int64_t run = 0;
+        for (int64_t n = 0; n * n_cta < n_all; ++n) {
+            const int64_t id = n * n_cta + ((n & 1) ? n_cta - 1 - b : b);
+            if (id >= n_all || items[id / H].n_keys == 0) continue;
+            if (items[id / H].rows <= 128) {
+                run += (items[id / H].n_keys + 127) / 128;
+            } else {
+                most = std::max(most, run);
+                run = 0;
+            }
+        }
+    }
+    return most;
+}
+
 // Test hook, host only: the launches of a problem on a GPU of n_sm SMs.  out: items of the forward's kernels (two query tiles, one, few
 // queries) that have keys, and rows to put together; items of dQ that have keys; pieces of dK/dV; slots of their sums; the longest
-// walk and the mean one of the two-tile launch, the one-tile launch and dQ, in key tiles
+// walk and the mean one of the two-tile launch, the one-tile launch and dQ, in key tiles; the longest wait in the first of these
 extern "C" int moc_debug_cross_plan(const moc_cross_problem *pr, int n_sm, int64_t *out) {
     if (!pr || !out) return MOC_ERR_NULL;
     if (int r = check_cross(pr)) return r;
@@ -590,6 +616,7 @@ extern "C" int moc_debug_cross_plan(const moc_cross_problem *pr, int n_sm, int64
     walks(c.items, c.H, n_sm, out + 7);
     walks(c.solo, c.H, n_sm, out + 9);
     walks(c.dq_items, c.H, n_sm, out + 11);
+    out[13] = longest_wait(c.items, c.H, n_sm);
     return MOC_OK;
 }
 

@@ -70,3 +70,15 @@ def test_more_than_can_be_counted_is_refused(case):
         plan(*case)
     assert e.value.code == -2
     assert plan(*case[:3], [300] * len(case[4]), case[4])["part_rows"] > 0
+
+
+@pytest.mark.parametrize("case", [
+    (64, 1, 64, [3_000_000] + [100] * 500, [1_000_000] + [1_100_000] * 500),
+    (8, 8, 128, [20_000_000] + [128] * 200 + [256], [300_000] + [900_000] * 200 + [50_000]),
+])
+def test_no_warp_waits_through_a_second_of_other_items(case):
+    """In items of one query tile the second tile's warps have nothing to do: their wait for the next of two is a bounded one, of two
+    seconds, some 600,000 key tiles at the lowest clock."""
+    p = plan(*case)
+    assert p["two_tile"] > 0 and p["one_tile"] == 0
+    assert p["two_tile_wait"] <= 300_000
