@@ -61,14 +61,41 @@ def _backward(x, w, a, b, cos, sin, dy):
     return r * (w * g - xh * m), size, (g * xh).sum(0), (gs * xh.abs()).sum(0)
 
 
+# the same of streams whose tokens several warps share, each with more than one batch: some with queries and keys
+SHARED = [
+    (2003, 24, 24, 128, (44, 42, 42), False, False, False),
+    (1999, 12, 24, 128, (32, 24, 24), True, False, False),
+    (1500, 24, 8, 128, (44, 42, 42), False, True, False),
+    (9001, 12, 12, 64, (16, 24, 24), False, False, True),
+    (6402, 12, 4, 64, (16, 16, 16), True, False, True),
+    (4001, 5, 9, 128, (44, 42, 42), False, True, True),
+]
+
+
+def _split(case, bwd):
+    L, hq, hk, d, _, _, fp32, _ = case
+    return debug_rope_split(fp32, bwd, d, L, hq, hk, torch.cuda.get_device_properties(0).multi_processor_count)
+
+
 @pytest.mark.parametrize("case", CASES)
 def test_walks_of_several_tokens(case):
-    L, hq, hk, d, ax, halves, fp32, by_token = case
-    n_sm = torch.cuda.get_device_properties(0).multi_processor_count
-    split = [debug_rope_split(fp32, bwd, d, L, hq, hk, n_sm) for bwd in (0, 1)]
+    split = [_split(case, bwd) for bwd in (0, 1)]
     for s in split:
-        assert s["by_token"] == by_token and s["per_warp"] > 1 and s["items"] > s["warps"]
+        assert s["by_token"] == case[-1] and s["per_warp"] > 1 and s["items"] > s["warps"]
     assert split[1]["items"] > 2 * split[1]["warps"]                     # a third token
+    _check(case, split[1])
+
+
+@pytest.mark.parametrize("case", SHARED)
+def test_tokens_that_several_warps_share(case):
+    split = [_split(case, bwd) for bwd in (0, 1)]
+    assert all(s["by_token"] == case[-1] for s in split) and any(s["n_split"] > 1 and s["per_warp"] > 1 for s in split)
+    _check(case, split[1])
+
+
+def _check(case, s):
+    """Both directions; s: the backward's split."""
+    L, hq, hk, d, ax, halves, fp32, _ = case
     x, w, pos, dy, axis, freq = _inputs(case, 1)
     op = MocRope.from_axes(d, ax, halves=halves)
     xv = x.transpose(0, 1)
@@ -82,7 +109,6 @@ def test_walks_of_several_tokens(case):
     half = R.U32 if fp32 else R.U16
     # A term of dw is off by the norm and the rotation's roundings, and goes through one sum after another: a lane's rows, a warp's lane
     # groups, eight warps, the blocks in 32 strands of eight at a time, and 32 strands.
-    s = split[1]
     rows = -(-s["items"] // s["warps"]) * s["per_warp"] * 6
     steps = rows + 2 + 8 + s["warps"] // 8 // 32 + 8 + 32
     for z, heads in ((0, range(hq)), (1, range(hq, hq + hk))):
